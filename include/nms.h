@@ -363,6 +363,116 @@ int nms_run_static_batched(const float *boxes, const float *scores, const int32_
 #define NMS_HOST_FORMS_DISAGREE (-100)
 int nms_host_pair_test(const float *victim, const float *outranking, float threshold);
 
+/*
+ * Decoding: which candidates of a model that answers in tokens stand.  The two choices of one decoding step, with the
+ * conventions above (device pointers, a stream, no state, nothing allocated, the same bits for the same inputs):
+ * how many drafted tokens stand against the target's probabilities (nms_verify_batched), and which rows of a cache
+ * stand by the attention weight that they gathered (nms_cache_keep_batched, nms_cache_move_batched, the whole path
+ * nms_cache_evict_batched).  The first says how many of the rows that a step wrote to the cache are valid; the second
+ * takes that as its counts, lengths and valid_tokens, and brings the cache back to its budget.
+ */
+enum { NMS_TYPE_F32 = 0, NMS_TYPE_F16 = 1, NMS_TYPE_BF16 = 2 };
+#define NMS_MAX_DRAFTS 1024          /* largest drafts_max accepted */
+#define NMS_MAX_VOCABULARY 4194304   /* largest vocabulary accepted */
+#define NMS_MAX_SLOTS 1048576        /* largest number of slots of a cache accepted */
+#define NMS_CACHE_MAX_TENSORS 8      /* tensors that one call moves */
+
+/*
+ * Verification of drafted tokens by given random numbers.  Sequence s has c = counts[s] drafted tokens x_0 .. x_(c-1);
+ * p_i and q_i are the target's and the draft's probabilities at place i, u its random numbers in [0, 1).
+ *   accepted   a = the first i < c for which  u_i * q_i(x_i) < p_i(x_i)  does not hold; c when all hold
+ *   weights    a < c:  w_j = max(p_a(j) - q_a(j), 0);   a = c:  w_j = p_c(j);   where all of them are 0:  w_j = p_a(j)
+ *   token      the least j with  w_0 + .. + w_j  >  u_(drafts_max) * (w_0 + .. + w_(V-1))
+ *   out        x_0 .. x_(a-1), token, -1 .. -1
+ * so that the tokens out are distributed as the target's own.  Products are exact and sums are in 64 bits (their order
+ * depends on the vocabulary alone, so a sequence's tokens do not depend on the batch); where rounding leaves no such j
+ * it is the last with w_j > 0; where p_a has no positive entry the token is -1.  Entries that are not a number, infinite
+ * or below 0 count as 0, and a drafted token outside the vocabulary has p = q = 0.
+ *   target   [sequences][drafts_max + 1][vocabulary] of `type`, target_stride elements from row to row
+ *   draft    [sequences][drafts_max][vocabulary] of `type`, draft_stride elements from row to row; NULL: the draft gave
+ *            tokens alone, q_i is 1 at x_i and 0 elsewhere
+ *   drafts   [sequences][drafts_max] int32 (may be NULL when drafts_max is 0: a plain draw from one row)
+ *   counts   [sequences] int32, values above drafts_max count as drafts_max; NULL: drafts_max everywhere.  Below 0: no
+ *            sequence at this place of the batch: nothing of it is read, accepted_out 0, tokens -1
+ *   uniforms [sequences][drafts_max + 1] float: drafts_max for the tests, the last for the token
+ *   tokens_out [sequences][drafts_max + 1] int32, accepted_out [sequences] int32
+ *   workspace  >= nms_verify_workspace_bytes(vocabulary, sequences) bytes, 256-byte aligned
+ * sequences == 0 is NMS_OK; vocabulary must be at least 1, strides at least vocabulary.
+ */
+size_t nms_verify_workspace_bytes(int vocabulary, int sequences);   /* host-only, pure; 0 on invalid arguments */
+int nms_verify_batched(const void *target, long long target_stride, const void *draft, long long draft_stride, int type,
+                       const int32_t *drafts, const int32_t *counts, int drafts_max, int vocabulary, int sequences,
+                       const float *uniforms, int32_t *tokens_out, int32_t *accepted_out, void *workspace, size_t ws_bytes,
+                       void *stream);
+
+/*
+ * Eviction from a cache by accumulated attention weight.  A sequence has n = counts[s] cached rows in slots 0 .. n-1 (the
+ * same number for each of its heads); per head and slot there are the weight gathered so far (sums) and the place of the
+ * row's token in the text (positions).
+ *   1  sums[i] += the step's attention weights of slot i, over the query heads that share the cached head and over the
+ *      step's valid tokens.  Added in 64 bits, rounded once to float; weights that are not finite add nothing.
+ *   2  the rows are ranked: protected rows first (position < first, or position >= lengths[s] - recent), then higher sums,
+ *      then lower slots; sums that are not a number come last.  Rows of rank below k = min(n, budget) stay.
+ *   3  the i-th row that stays in a slot at or beyond k moves to the i-th slot below k whose row does not: the rows that
+ *      stay fill slots 0 .. k-1, and no other row is touched.  Slots keep no order of positions; whole pages at or beyond
+ *      slot k are free.
+ * nms_cache_keep_batched does 1 and 2 and names the moves of 3, nms_cache_move_batched moves rows of the caller's tensors,
+ * and nms_cache_evict_batched does all of it, moves sums and positions as well and sets the sums of slots k .. n-1 to 0 (so
+ * that the next rows written there start with none).  Slots at or beyond n are left as they are in every buffer but keep_out.
+ *   sums       float [sequences][heads][n_max], in and out
+ *   positions  int32 [sequences][heads][n_max] (out in the whole path), NULL: the slot's number (in the whole path only with
+ *              recent == 0, since rows move)
+ *   counts     [sequences] int32, clamped to [0, n_max]; NULL: n_max
+ *   lengths    [sequences] int32, the tokens of the text so far; NULL: counts
+ *   weights    HOST pointer, or NULL (nothing is added)
+ *   keep_out   [sequences][heads][n_max] bytes, 1 = the row of this slot stays (slots as before any move), 0 = it goes or
+ *              there is none; NULL: not wanted
+ *   kept_out   [sequences] int32, k: the next step's rows are written behind it (a buffer other than counts); NULL: not wanted
+ *   moves_out  int32 [sequences][heads][nms_cache_moves_max(n_max, budget) + 1][2]: the number of moves and 0, then pairs
+ *              (to, from), to ascending, from ascending; entries behind them are left as they are; NULL: not wanted
+ *   workspace  >= nms_cache_workspace_bytes(n_max, heads, sequences, budget) bytes, 256-byte aligned
+ * n_max <= NMS_MAX_SLOTS, sequences * heads <= NMS_MAX_FRAMES, budget, first and recent >= 0.
+ */
+typedef struct nms_cache_weights {
+    const void *weights;          /* device [sequences][heads][group][tokens][columns] of `type`, row_stride elements from row to row */
+    long long row_stride;         /* >= columns */
+    int32_t type;                 /* NMS_TYPE_* */
+    int32_t group;                /* query heads that share a cached head, >= 1 */
+    int32_t tokens;               /* query rows per query head, >= 1 */
+    int32_t columns;              /* slots that have a weight; those at or beyond it get none */
+    const int32_t *valid_tokens;  /* device [sequences]: how many of the query rows count, from the first (clamped to [0, tokens]); NULL: all */
+} nms_cache_weights;
+/* A tensor whose rows move with their slots: row (sequence, head, slot) begins at rows + sequence * sequence_stride +
+ * head * head_stride + slot * slot_stride, all in bytes, in any order of size; rows must not overlap.  With pages it begins at rows +
+ * page * sequence_stride + head * head_stride + (slot % page_slots) * slot_stride, page = table[sequence * table_stride + slot / page_slots]. */
+typedef struct nms_cache_tensor {
+    void *rows;                /* device */
+    long long row_bytes;       /* 1 .. 2^20 */
+    long long sequence_stride; /* with pages: from page to page */
+    long long head_stride;
+    long long slot_stride;
+} nms_cache_tensor;
+typedef struct nms_cache_pages {
+    const int32_t *table;      /* device [sequences][table_stride] page numbers; a move from or to a page outside 0 .. pages-1 is left out */
+    int32_t table_stride;      /* >= ceil(n_max / page_slots) */
+    int32_t page_slots;        /* >= 1 */
+    int32_t pages;             /* pages that the tensors hold */
+    int32_t reserved;          /* must be 0 */
+} nms_cache_pages;
+int nms_cache_moves_max(int n_max, int budget);   /* host-only, pure: min(budget, n_max - budget), at least 0; -1 on invalid arguments */
+size_t nms_cache_workspace_bytes(int n_max, int heads, int sequences, int budget);   /* host-only, pure; 0 on invalid arguments */
+int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t *counts, const int32_t *lengths, int n_max,
+                           int heads, int sequences, const nms_cache_weights *weights, int budget, int first, int recent,
+                           uint8_t *keep_out, int32_t *kept_out, int32_t *moves_out, void *workspace, size_t ws_bytes, void *stream);
+/* Moves rows as moves_out of nms_cache_keep_batched says (same n_max, heads, sequences and budget); a pair outside the slots that such a
+ * list can name is left out.  `tensors` is a HOST array of n_tensors <= NMS_CACHE_MAX_TENSORS, `pages` a HOST pointer or NULL. */
+int nms_cache_move_batched(const int32_t *moves, int n_max, int heads, int sequences, int budget, const nms_cache_tensor *tensors,
+                           int n_tensors, const nms_cache_pages *pages, void *stream);
+int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *counts, const int32_t *lengths, int n_max,
+                            int heads, int sequences, const nms_cache_weights *weights, int budget, int first, int recent,
+                            const nms_cache_tensor *tensors, int n_tensors, const nms_cache_pages *pages,
+                            uint8_t *keep_out, int32_t *kept_out, void *workspace, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,9 @@ _BINDING_NAMES = (
     "nms_run_batched_profiled", "nms_reduce_greedy", "nms_reduce_greedy_batched",
     "nms_greedy_workspace_bytes", "nms_run_greedy_batched", "nms_run_greedy_fused_batched", "nms_run_early_exit_batched", "nms_map_matrix", "nms_reduce_matrix", "nms_ex_workspace_bytes", "nms_run_ex_batched", "NmsOptions",
     "nms_init", "nms_shutdown", "nms_run", "nms_run_static_batched", "NMS_STATIC_SCRATCH_BYTES",
+    "nms_verify_workspace_bytes", "nms_verify_batched", "VerifyPlan",
+    "nms_cache_moves_max", "nms_cache_workspace_bytes", "nms_cache_keep_batched", "nms_cache_move_batched", "nms_cache_evict_batched", "CachePlan",
+    "NMS_TYPE_F32", "NMS_TYPE_F16", "NMS_TYPE_BF16", "NMS_MAX_DRAFTS", "NMS_MAX_VOCABULARY", "NMS_MAX_SLOTS", "NMS_CACHE_MAX_TENSORS",
 )
 
 __all__ = list(_BINDING_NAMES)

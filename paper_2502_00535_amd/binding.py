@@ -34,6 +34,8 @@ EXPORTS = (
     "nms_greedy_workspace_bytes", "nms_run_greedy_batched", "nms_run_greedy_fused_batched", "nms_run_early_exit_batched", "nms_map_matrix", "nms_reduce_matrix",
     "nms_ex_workspace_bytes", "nms_run_ex_batched",
     "nms_init", "nms_shutdown", "nms_run", "nms_run_static_batched", "nms_host_pair_test",
+    "nms_verify_workspace_bytes", "nms_verify_batched", "nms_cache_moves_max", "nms_cache_workspace_bytes",
+    "nms_cache_keep_batched", "nms_cache_move_batched", "nms_cache_evict_batched",
 )
 
 
@@ -42,6 +44,25 @@ class NmsOptions(ctypes.Structure):
     _fields_ = [("rule", ctypes.c_int32), ("measure", ctypes.c_int32), ("compare", ctypes.c_int32),
                 ("ties", ctypes.c_int32), ("pixel_offset", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("classes", ctypes.c_void_p)]
+
+
+class NmsCacheWeights(ctypes.Structure):
+    """struct nms_cache_weights of include/nms.h."""
+    _fields_ = [("weights", ctypes.c_void_p), ("row_stride", ctypes.c_longlong), ("type", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("tokens", ctypes.c_int32), ("columns", ctypes.c_int32),
+                ("valid_tokens", ctypes.c_void_p)]
+
+
+class NmsCacheTensor(ctypes.Structure):
+    """struct nms_cache_tensor of include/nms.h."""
+    _fields_ = [("rows", ctypes.c_void_p), ("row_bytes", ctypes.c_longlong), ("sequence_stride", ctypes.c_longlong),
+                ("head_stride", ctypes.c_longlong), ("slot_stride", ctypes.c_longlong)]
+
+
+class NmsCachePages(ctypes.Structure):
+    """struct nms_cache_pages of include/nms.h."""
+    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int32), ("page_slots", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 RULES = {"paper": 0, "greedy": 1}
@@ -136,6 +157,23 @@ def _load() -> ctypes.CDLL:
     L.nms_run.argtypes = [vp, vp, i32, f32, vp, vp]
     L.nms_run_static_batched.restype = i32
     L.nms_run_static_batched.argtypes = [vp, vp, vp, i32, i32, f32, vp, vp]
+    i64 = ctypes.c_longlong
+    L.nms_verify_workspace_bytes.restype = sz
+    L.nms_verify_workspace_bytes.argtypes = [i32, i32]
+    L.nms_verify_batched.restype = i32
+    L.nms_verify_batched.argtypes = [vp, i64, vp, i64, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    L.nms_cache_moves_max.restype = i32
+    L.nms_cache_moves_max.argtypes = [i32, i32]
+    L.nms_cache_workspace_bytes.restype = sz
+    L.nms_cache_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    weights_p, tensor_p, pages_p = (ctypes.POINTER(s) for s in (NmsCacheWeights, NmsCacheTensor, NmsCachePages))
+    L.nms_cache_keep_batched.restype = i32
+    L.nms_cache_keep_batched.argtypes = [vp, vp, vp, vp, i32, i32, i32, weights_p, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    L.nms_cache_move_batched.restype = i32
+    L.nms_cache_move_batched.argtypes = [vp, i32, i32, i32, i32, tensor_p, i32, pages_p, vp]
+    L.nms_cache_evict_batched.restype = i32
+    L.nms_cache_evict_batched.argtypes = [vp, vp, vp, vp, i32, i32, i32, weights_p, i32, i32, i32, tensor_p, i32, pages_p,
+                                          vp, vp, vp, sz, vp]
     L.nms_host_pair_test.restype = i32
     L.nms_host_pair_test.argtypes = [ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_float), f32]
     return L
@@ -525,3 +563,235 @@ def nms_run_static_batched(boxes, scores, counts, n_max, frames, threshold, keep
                                       _ptr(counts, "int32", "counts", int(frames)), int(n_max), int(frames), float(threshold),
                                       _ptr(keep_out, "uint8", "keep_out", fn_), _stream(stream)),
            "nms_run_static_batched")
+
+
+# ------------------------------------------------------------------ the choices of a decoding step
+
+NMS_TYPE_F32, NMS_TYPE_F16, NMS_TYPE_BF16 = 0, 1, 2
+NMS_MAX_FRAMES, NMS_MAX_DRAFTS, NMS_MAX_VOCABULARY, NMS_MAX_SLOTS, NMS_CACHE_MAX_TENSORS = 65535, 1024, 4194304, 1048576, 8
+_TYPES = {torch.float32: NMS_TYPE_F32, torch.float16: NMS_TYPE_F16, torch.bfloat16: NMS_TYPE_BF16}
+
+
+def _here(**tensors):
+    """The kernels run on the current device: tensors of another one are refused."""
+    for what, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{what}: tensor lives on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _strided(t, what):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a torch tensor")
+    if not _on_device(t):
+        raise ValueError(f"{what}: tensor must live on the GPU")
+    return t
+
+
+def _type_of(t, what):
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{what}: expected float32, float16 or bfloat16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _rows(t, shape, what):
+    """(address, stride from row to row) of a tensor whose leading dimensions are `shape` but the last, and whose last holds at least
+    shape[-1] neighbouring elements: rows may lie apart, all at one distance."""
+    t = _strided(t, what)
+    if t.dim() != len(shape) or tuple(t.shape[:-1]) != tuple(shape[:-1]) or t.shape[-1] < shape[-1]:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, the call needs {tuple(shape)}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be neighbours")
+    row, expect = None, None
+    for d in range(len(shape) - 2, -1, -1):
+        if shape[d] == 1:
+            continue
+        if row is None:
+            row = expect = t.stride(d)
+        if t.stride(d) != expect:
+            raise ValueError(f"{what}: rows must lie at one distance from each other")
+        expect *= shape[d]
+    if row is None:
+        row = shape[-1]
+    if row < shape[-1]:
+        raise ValueError(f"{what}: rows must not overlap")
+    return t.data_ptr(), row
+
+
+def nms_verify_workspace_bytes(vocabulary: int, sequences: int) -> int:
+    return int(lib.nms_verify_workspace_bytes(int(vocabulary), int(sequences)))
+
+
+def _verify_arguments(target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace):
+    k, v, s = int(drafts_max), int(vocabulary), int(sequences)
+    _here(target=target, draft=draft, drafts=drafts, counts=counts, uniforms=uniforms, tokens_out=tokens_out,
+          accepted_out=accepted_out, workspace=workspace)
+    t_at, t_row, d_at, d_row, kind = None, v, None, v, NMS_TYPE_F32
+    if 0 <= k <= NMS_MAX_DRAFTS and 1 <= v <= NMS_MAX_VOCABULARY and 1 <= s <= NMS_MAX_FRAMES:  # else the library refuses the sizes, or there is nothing to do
+        t_at, t_row = _rows(target, (s, k + 1, v), "target")
+        kind = _type_of(target, "target")
+        if draft is not None and k > 0:
+            d_at, d_row = _rows(draft, (s, k, v), "draft")
+            if draft.dtype != target.dtype:
+                raise TypeError(f"draft: expected dtype {target.dtype}, got {draft.dtype}")
+    need = max(s, 0) * (max(k, 0) + 1)
+    w, wb = _ws(workspace)
+    return (t_at, t_row, d_at, d_row, kind, _ptr(drafts, "int32", "drafts", max(s, 0) * max(k, 0)), _ptr(counts, "int32", "counts", max(s, 0)),
+            k, v, s, _ptr(uniforms, "float32", "uniforms", need), _ptr(tokens_out, "int32", "tokens_out", need),
+            _ptr(accepted_out, "int32", "accepted_out", max(s, 0)), w, wb)
+
+
+def nms_verify_batched(target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace,
+                       stream=None):
+    """target: [sequences, drafts_max + 1, >= vocabulary]; draft: [sequences, drafts_max, >= vocabulary] of the same dtype, or None.
+    Their rows may lie apart (a slice of wider rows), all at one distance."""
+    _check(lib.nms_verify_batched(*_verify_arguments(target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms,
+                                                     tokens_out, accepted_out, workspace), _stream(stream)), "nms_verify_batched")
+
+
+def nms_cache_moves_max(n_max: int, budget: int) -> int:
+    return int(lib.nms_cache_moves_max(int(n_max), int(budget)))
+
+
+def nms_cache_workspace_bytes(n_max: int, heads: int, sequences: int, budget: int) -> int:
+    return int(lib.nms_cache_workspace_bytes(int(n_max), int(heads), int(sequences), int(budget)))
+
+
+def _cache_elements(n_max, heads, sequences):
+    """sequences * heads * n_max and sequences; zeros when the library will refuse the sizes anyway."""
+    if n_max < 0 or heads < 0 or sequences < 0 or n_max > NMS_MAX_SLOTS or heads * sequences > NMS_MAX_FRAMES:
+        return 0, 0
+    return sequences * heads * n_max, sequences
+
+
+def _cache_weights(weights, valid_tokens, heads, sequences):
+    """struct nms_cache_weights of a tensor [sequences, heads, group, tokens, columns], or None."""
+    if weights is None:
+        return None
+    weights = _strided(weights, "weights")
+    if weights.dim() != 5 or weights.shape[0] != sequences or weights.shape[1] != heads:
+        raise ValueError(f"weights: shape {tuple(weights.shape)}, the call needs ({sequences}, {heads}, group, tokens, columns)")
+    at, row = _rows(weights, tuple(weights.shape), "weights")
+    return NmsCacheWeights(at, row, _type_of(weights, "weights"), weights.shape[2], weights.shape[3], weights.shape[4],
+                           _ptr(valid_tokens, "int32", "valid_tokens", sequences))
+
+
+def _cache_tensors(tensors, n_max, heads, sequences, page_table):
+    """Array of struct nms_cache_tensor, and struct nms_cache_pages or None."""
+    tensors = list(tensors or ())
+    structs, shape = (NmsCacheTensor * max(len(tensors), 1))(), None
+    for i, t in enumerate(tensors):
+        what = f"tensors[{i}]"
+        t = _strided(t, what)
+        if t.dim() < 3 or t.shape[1] < heads or (page_table is None and (t.shape[0] < sequences or t.shape[2] < n_max)):
+            need = f"({sequences}, {heads}, {n_max}, ...)" if page_table is None else f"(pages, {heads}, slots of a page, ...)"
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, the call needs {need}")
+        row = 1
+        for d in range(t.dim() - 1, 2, -1):
+            if t.shape[d] != 1 and t.stride(d) != row:
+                raise ValueError(f"{what}: the elements of a row must be neighbours")
+            row *= t.shape[d]
+        extent = row
+        for stride, size in sorted((t.stride(d), t.shape[d]) for d in range(3)):
+            if size > 1:
+                if stride < extent:
+                    raise ValueError(f"{what}: rows must not overlap")
+                extent += stride * (size - 1)
+        if shape is None:
+            shape = (t.shape[0], t.shape[2])
+        elif page_table is not None and shape != (t.shape[0], t.shape[2]):
+            raise ValueError(f"{what}: pages of the tensors must be as many and as long")
+        b = t.element_size()
+        structs[i] = NmsCacheTensor(t.data_ptr(), row * b, t.stride(0) * b, t.stride(1) * b, t.stride(2) * b)
+    if page_table is None or not tensors:
+        return structs, len(tensors), None
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] < sequences:
+        raise ValueError(f"page_table: expected a tensor ({sequences}, pages of a sequence)")
+    each = -(-max(n_max, 0) // max(shape[1], 1))
+    if page_table.shape[1] < each:
+        raise ValueError(f"page_table: {page_table.shape[1]} pages to a sequence, the call needs {each}")
+    at = _ptr(page_table, "int32", "page_table", 0)
+    return structs, len(tensors), NmsCachePages(at, page_table.shape[1], shape[1], shape[0], 0)
+
+
+def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, keep_out, kept_out, moves_out,
+                           workspace, weights=None, valid_tokens=None, stream=None):
+    """weights: [sequences, heads, group, tokens, columns], rows at one distance from each other, or None.
+    moves_out: at least sequences * heads * (nms_cache_moves_max(n_max, budget) + 1) * 2 elements, or None."""
+    n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
+    _here(sums=sums, positions=positions, counts=counts, lengths=lengths, keep_out=keep_out, kept_out=kept_out, moves_out=moves_out,
+          workspace=workspace, weights=weights, valid_tokens=valid_tokens)
+    all_, s_ = _cache_elements(n, h, s)
+    w, wb = _ws(workspace)
+    struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
+    _check(lib.nms_cache_keep_batched(
+        _ptr(sums, "float32", "sums", all_), _ptr(positions, "int32", "positions", all_), _ptr(counts, "int32", "counts", s_),
+        _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, int(first), int(recent), _ptr(keep_out, "uint8", "keep_out", all_),
+        _ptr(kept_out, "int32", "kept_out", s_),
+        _ptr(moves_out, "int32", "moves_out", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ else 0), w, wb, _stream(stream)),
+        "nms_cache_keep_batched")
+
+
+def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page_table=None, stream=None):
+    """tensors: up to eight of shape [sequences, heads, n_max, row ...] (any strides whose rows are whole), or with a page table
+    ([sequences, pages of a sequence] int32) [pages, heads, slots of a page, row ...]."""
+    n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
+    _here(moves=moves, page_table=page_table, **{f"tensors[{i}]": t for i, t in enumerate(tensors or ())})
+    all_, s_ = _cache_elements(n, h, s)
+    structs, many, pages = _cache_tensors(tensors, n, h, s, page_table)
+    _check(lib.nms_cache_move_batched(_ptr(moves, "int32", "moves", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ else 0),
+                                      n, h, s, b, structs, many, pages, _stream(stream)), "nms_cache_move_batched")
+
+
+def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
+                     workspace, weights, valid_tokens, page_table):
+    n, h, s = int(n_max), int(heads), int(sequences)
+    _here(sums=sums, positions=positions, counts=counts, lengths=lengths, keep_out=keep_out, kept_out=kept_out, workspace=workspace,
+          weights=weights, valid_tokens=valid_tokens, page_table=page_table, **{f"tensors[{i}]": t for i, t in enumerate(tensors or ())})
+    all_, s_ = _cache_elements(n, h, s)
+    w, wb = _ws(workspace)
+    struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
+    structs, many, pages = _cache_tensors(tensors if all_ else (), n, h, s, page_table)
+    return (_ptr(sums, "float32", "sums", all_), _ptr(positions, "int32", "positions", all_), _ptr(counts, "int32", "counts", s_),
+            _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, int(budget), int(first), int(recent), structs, many, pages,
+            _ptr(keep_out, "uint8", "keep_out", all_), _ptr(kept_out, "int32", "kept_out", s_), w, wb)
+
+
+def nms_cache_evict_batched(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
+                            workspace, weights=None, valid_tokens=None, page_table=None, stream=None):
+    """The whole path: tensors and page_table as nms_cache_move_batched takes them, the rest as nms_cache_keep_batched."""
+    _check(lib.nms_cache_evict_batched(*_evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent,
+                                                         tensors, keep_out, kept_out, workspace, weights, valid_tokens, page_table),
+                                       _stream(stream)), "nms_cache_evict_batched")
+
+
+class _DecodingPlan:
+    """A call with its arguments marshalled once, for decoding loops whose buffers stay: each call is then a single foreign call.
+    The plan holds references to its tensors; a call uses the stream given here, or the current one of the device that the plan was
+    made on, which must be the current device."""
+
+    def __init__(self, entry, args, keepalive, stream):
+        self._entry, self._fn, self._args, self._keepalive, self._given = entry, getattr(lib, entry), args, keepalive, stream
+
+    def __call__(self):
+        status = self._fn(*self._args, _stream(self._given))
+        if status != NMS_OK:
+            raise NmsError(status, self._entry)
+
+
+class VerifyPlan(_DecodingPlan):
+    """nms_verify_batched, marshalled once."""
+
+    def __init__(self, target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace,
+                 stream=None):
+        args = (target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace)
+        super().__init__("nms_verify_batched", _verify_arguments(*args), args, stream)
+
+
+class CachePlan(_DecodingPlan):
+    """nms_cache_evict_batched, marshalled once."""
+
+    def __init__(self, sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
+                 workspace, weights=None, valid_tokens=None, page_table=None, stream=None):
+        args = (sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tuple(tensors or ()), keep_out, kept_out,
+                workspace, weights, valid_tokens, page_table)
+        super().__init__("nms_cache_evict_batched", _evict_arguments(*args), args, stream)

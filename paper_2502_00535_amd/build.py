@@ -7,8 +7,9 @@ import sysconfig
 import warnings
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(_HERE, "csrc", "nms_kernels.hip")]
+SOURCES = [os.path.join(_HERE, "csrc", "nms_kernels.hip"), os.path.join(_HERE, "csrc", "decoding_kernels.hip")]
 HEADERS = [os.path.join(_HERE, "csrc", "nms_pair.h"), os.path.join(_HERE, "csrc", "nms_host_logic.h"), os.path.join(_HERE, "csrc", "nms_place.h"),
+           os.path.join(_HERE, "csrc", "nms_launch.h"), os.path.join(_HERE, "csrc", "nms_decoding_logic.h"),
            os.path.join(os.path.dirname(_HERE), "include", "nms.h"),
            *sorted(os.path.join(_HERE, "csrc", "kernels", f)
                    for f in os.listdir(os.path.join(_HERE, "csrc", "kernels")) if f.endswith(".h"))]
@@ -62,18 +63,32 @@ def build_marshal_if_possible() -> str | None:
         return None
 
 
+def _hipcc(*commands) -> list[str]:
+    """Runs the commands side by side; returns what each wrote to stderr."""
+    procs = [subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True) for cmd in commands]
+    said = [proc.communicate() for proc in procs]  # every one ends before the first failure is raised
+    for proc, (out, err) in zip(procs, said):
+        if proc.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + " ".join(proc.args) + "\n" + out + err)
+    return [err for _, err in said]
+
+
 def build_library(verbose: bool = False) -> str:
     """Always compiles (the binding's marshalling module as well, where that can be done); returns the path of the shared object."""
     build_marshal_if_possible()
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIBRARY + f".tmp{os.getpid()}"
-    cmd = [hipcc, *HIPCC_FLAGS, *SOURCES, "-o", tmp]
-    proc = subprocess.run(cmd, capture_output=True, text=True)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + proc.stdout + proc.stderr)
+    objects = [tmp + f".{i}.o" for i in range(len(SOURCES))]
+    try:
+        messages = _hipcc(*([hipcc, *HIPCC_FLAGS, "-c", source, "-o", obj] for source, obj in zip(SOURCES, objects)))
+        messages += _hipcc([hipcc, *HIPCC_FLAGS, *objects, "-o", tmp])
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     if verbose:
         # the host pass does not know the device-only target feature; that warning is expected
-        print("\n".join(l for l in proc.stderr.splitlines() if "not a recognized feature" not in l))
+        print("\n".join(l for m in messages for l in m.splitlines() if "not a recognized feature" not in l))
     os.replace(tmp, LIBRARY)
     return LIBRARY
 

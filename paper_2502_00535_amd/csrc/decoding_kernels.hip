@@ -1,0 +1,212 @@
+// The choices of a decoding step (gfx950, wave64): how many drafted tokens stand, and which rows of a cache stay.
+//
+// As for boxes, candidates have scores, the order is total (higher score, then lower index), and the outcome says which of
+// them stand.  The kernels live in kernels/verify.h, kernels/cache_keep.h and kernels/cache_move.h (included below inside the
+// anonymous namespace); the launch logic and the extern "C" entry points follow.
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include "nms_decoding_logic.h"
+#include "nms_launch.h"
+
+namespace {
+
+struct bf16_bits { uint16_t u; };
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(_Float16 v) { return (float)v; }
+__device__ __forceinline__ float to_float(bf16_bits v) { return __uint_as_float((unsigned)v.u << 16); }
+
+__device__ __forceinline__ int frame_count(const int32_t *counts, int s, int n_max)
+{
+    if (counts == nullptr) return n_max;
+    const int c = counts[s];
+    return c < 0 ? 0 : (c > n_max ? n_max : c);
+}
+
+#include "kernels/verify.h"
+#include "kernels/cache_keep.h"
+#include "kernels/cache_move.h"
+
+// ----------------------------------------------------------------------------- host side
+
+inline bool known_type(int type) { return type == NMS_TYPE_F32 || type == NMS_TYPE_F16 || type == NMS_TYPE_BF16; }
+
+inline int workspace_status(const void *workspace, size_t ws_bytes, size_t need)
+{
+    if (need == 0) return NMS_OK;
+    return workspace == nullptr || (uintptr_t)workspace % 256 != 0 || ws_bytes < need ? NMS_ERR_WORKSPACE : NMS_OK;
+}
+
+template <typename T>
+void verify_launch(const VerifyArgs &a, int sequences, hipStream_t stream)
+{
+    if (a.draft != nullptr) verify_kernel<T, true><<<dim3(sequences), dim3(kVerifyThreads), 0, stream>>>(a);
+    else verify_kernel<T, false><<<dim3(sequences), dim3(kVerifyThreads), 0, stream>>>(a);
+}
+
+int cache_sizes_status(int n_max, int heads, int sequences, int budget)
+{
+    if (n_max < 0 || heads < 0 || sequences < 0 || budget < 0) return NMS_ERR_INVALID_ARG;
+    if (n_max > NMS_MAX_SLOTS || (long long)heads * sequences > NMS_MAX_FRAMES) return NMS_ERR_TOO_LARGE;
+    return NMS_OK;
+}
+
+int weights_status(const nms_cache_weights *w)
+{
+    if (w == nullptr) return NMS_OK;
+    if (!known_type(w->type) || w->group < 0 || w->tokens < 0 || w->columns < 0 || w->row_stride < w->columns) return NMS_ERR_INVALID_ARG;
+    if (w->weights == nullptr && w->group > 0 && w->tokens > 0 && w->columns > 0) return NMS_ERR_INVALID_ARG;
+    return NMS_OK;
+}
+
+int tensors_status(const nms_cache_tensor *tensors, int n_tensors, const nms_cache_pages *pages, int n_max)
+{
+    if (n_tensors < 0 || (n_tensors > 0 && tensors == nullptr)) return NMS_ERR_INVALID_ARG;
+    if (n_tensors > NMS_CACHE_MAX_TENSORS) return NMS_ERR_TOO_LARGE;
+    for (int i = 0; i < n_tensors; ++i)
+        if (tensors[i].rows == nullptr || tensors[i].row_bytes < 1 || tensors[i].row_bytes > (1 << 20)) return NMS_ERR_INVALID_ARG;
+    if (pages == nullptr) return NMS_OK;
+    if (pages->table == nullptr || pages->page_slots < 1 || pages->pages < 0 || pages->reserved != 0) return NMS_ERR_INVALID_ARG;
+    return (long long)pages->table_stride * pages->page_slots < n_max ? NMS_ERR_INVALID_ARG : NMS_OK;
+}
+
+int add_launch(const CacheArgs &a, const nms_cache_weights *w, int frames, hipStream_t stream)
+{
+    if (w == nullptr || w->group == 0 || w->tokens == 0 || w->columns == 0) return NMS_OK;
+    const WeightArgs args = {w->weights, w->row_stride, w->valid_tokens, w->group, w->tokens, w->columns};
+    const int columns = w->columns < a.n_max ? w->columns : a.n_max;
+    const dim3 grid((columns + 255) / 256, frames), block(256);
+    begin_launch();
+    if (w->type == NMS_TYPE_F32) cache_add_kernel<float><<<grid, block, 0, stream>>>(a, args);
+    else if (w->type == NMS_TYPE_F16) cache_add_kernel<_Float16><<<grid, block, 0, stream>>>(a, args);
+    else cache_add_kernel<bf16_bits><<<grid, block, 0, stream>>>(a, args);
+    return launch_status();
+}
+
+int keep_launch(const CacheArgs &a, const nms_cache_weights *w, int frames, hipStream_t stream)
+{
+    const int st = add_launch(a, w, frames, stream);
+    if (st != NMS_OK) return st;
+    begin_launch();
+    cache_keep_kernel<<<dim3(frames), dim3(kKeepThreads), 0, stream>>>(a);
+    return launch_status();
+}
+
+int move_launch(const int32_t *moves, int n_max, int heads, int frames, int budget, const nms_cache_tensor *tensors, int n_tensors,
+                const nms_cache_pages *pages, hipStream_t stream)
+{
+    MoveArgs m = {};
+    m.moves = moves, m.n_max = n_max, m.heads = heads, m.budget = budget, m.moves_max = nms_moves_max(n_max, budget), m.n_tensors = n_tensors;
+    if (m.moves_max == 0 || n_tensors == 0) return NMS_OK;
+    if (pages != nullptr) m.pages = *pages;
+    for (int i = 0; i < n_tensors; ++i) {
+        m.tensors[i].t = tensors[i];
+        m.tensors[i].piece = nms_cache_piece(tensors[i]);
+        m.tensors[i].pieces = (int)(tensors[i].row_bytes / m.tensors[i].piece);
+    }
+    begin_launch();
+    cache_move_kernel<<<dim3((m.moves_max + kMoveRows - 1) / kMoveRows, frames), dim3(256), 0, stream>>>(m);
+    return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t nms_verify_workspace_bytes(int vocabulary, int sequences)
+{
+    if (vocabulary < 1 || vocabulary > NMS_MAX_VOCABULARY || sequences < 0 || sequences > NMS_MAX_FRAMES) return 0;
+    return 0;
+}
+
+int nms_verify_batched(const void *target, long long target_stride, const void *draft, long long draft_stride, int type,
+                       const int32_t *drafts, const int32_t *counts, int drafts_max, int vocabulary, int sequences,
+                       const float *uniforms, int32_t *tokens_out, int32_t *accepted_out, void *workspace, size_t ws_bytes,
+                       void *stream)
+{
+    if (!known_type(type) || drafts_max < 0 || vocabulary < 1 || sequences < 0 || target_stride < vocabulary ||
+        (draft != nullptr && drafts_max > 0 && draft_stride < vocabulary))
+        return NMS_ERR_INVALID_ARG;
+    if (drafts_max > NMS_MAX_DRAFTS || vocabulary > NMS_MAX_VOCABULARY || sequences > NMS_MAX_FRAMES) return NMS_ERR_TOO_LARGE;
+    if (sequences == 0) return NMS_OK;
+    if (target == nullptr || (drafts == nullptr && drafts_max > 0) || uniforms == nullptr || tokens_out == nullptr || accepted_out == nullptr)
+        return NMS_ERR_INVALID_ARG;
+    const int st = workspace_status(workspace, ws_bytes, nms_verify_workspace_bytes(vocabulary, sequences));
+    if (st != NMS_OK) return st;
+    const VerifyArgs a = {target, draft, target_stride, draft_stride, drafts, counts, uniforms, tokens_out, accepted_out, drafts_max, vocabulary};
+    begin_launch();
+    if (type == NMS_TYPE_F32) verify_launch<float>(a, sequences, static_cast<hipStream_t>(stream));
+    else if (type == NMS_TYPE_F16) verify_launch<_Float16>(a, sequences, static_cast<hipStream_t>(stream));
+    else verify_launch<bf16_bits>(a, sequences, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+int nms_cache_moves_max(int n_max, int budget)
+{
+    if (n_max < 0 || n_max > NMS_MAX_SLOTS || budget < 0) return -1;
+    return nms_moves_max(n_max, budget);
+}
+
+size_t nms_cache_workspace_bytes(int n_max, int heads, int sequences, int budget)
+{
+    if (cache_sizes_status(n_max, heads, sequences, budget) != NMS_OK) return 0;
+    return nms_cache_scratch(n_max, heads * sequences, budget);
+}
+
+int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t *counts, const int32_t *lengths, int n_max,
+                           int heads, int sequences, const nms_cache_weights *weights, int budget, int first, int recent,
+                           uint8_t *keep_out, int32_t *kept_out, int32_t *moves_out, void *workspace, size_t ws_bytes, void *stream)
+{
+    int st = cache_sizes_status(n_max, heads, sequences, budget);
+    if (st != NMS_OK) return st;
+    if (first < 0 || recent < 0) return NMS_ERR_INVALID_ARG;
+    st = weights_status(weights);
+    if (st != NMS_OK) return st;
+    if (n_max == 0 || heads == 0 || sequences == 0) return NMS_OK;
+    if (sums == nullptr) return NMS_ERR_INVALID_ARG;
+    st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
+    if (st != NMS_OK) return st;
+    const CacheArgs a = {sums, const_cast<int32_t *>(positions), counts, lengths, keep_out, kept_out, moves_out, n_max, heads, budget, first, recent,
+                         nms_moves_max(n_max, budget), false};
+    return keep_launch(a, weights, heads * sequences, static_cast<hipStream_t>(stream));
+}
+
+int nms_cache_move_batched(const int32_t *moves, int n_max, int heads, int sequences, int budget, const nms_cache_tensor *tensors,
+                           int n_tensors, const nms_cache_pages *pages, void *stream)
+{
+    int st = cache_sizes_status(n_max, heads, sequences, budget);
+    if (st != NMS_OK) return st;
+    st = tensors_status(tensors, n_tensors, pages, n_max);
+    if (st != NMS_OK) return st;
+    if (n_max == 0 || heads == 0 || sequences == 0 || n_tensors == 0) return NMS_OK;
+    if (moves == nullptr) return NMS_ERR_INVALID_ARG;
+    return move_launch(moves, n_max, heads, heads * sequences, budget, tensors, n_tensors, pages, static_cast<hipStream_t>(stream));
+}
+
+int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *counts, const int32_t *lengths, int n_max,
+                            int heads, int sequences, const nms_cache_weights *weights, int budget, int first, int recent,
+                            const nms_cache_tensor *tensors, int n_tensors, const nms_cache_pages *pages,
+                            uint8_t *keep_out, int32_t *kept_out, void *workspace, size_t ws_bytes, void *stream)
+{
+    int st = cache_sizes_status(n_max, heads, sequences, budget);
+    if (st != NMS_OK) return st;
+    if (first < 0 || recent < 0 || (positions == nullptr && recent > 0)) return NMS_ERR_INVALID_ARG;
+    st = weights_status(weights);
+    if (st != NMS_OK) return st;
+    st = tensors_status(tensors, n_tensors, pages, n_max);
+    if (st != NMS_OK) return st;
+    if (n_max == 0 || heads == 0 || sequences == 0) return NMS_OK;
+    if (sums == nullptr) return NMS_ERR_INVALID_ARG;
+    st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
+    if (st != NMS_OK) return st;
+    const int frames = heads * sequences;
+    int32_t *moves = static_cast<int32_t *>(workspace);
+    const CacheArgs a = {sums, positions, counts, lengths, keep_out, kept_out, moves, n_max, heads, budget, first, recent,
+                         nms_moves_max(n_max, budget), true};
+    st = keep_launch(a, weights, frames, static_cast<hipStream_t>(stream));
+    if (st != NMS_OK) return st;
+    return move_launch(moves, n_max, heads, frames, budget, tensors, n_tensors, pages, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,65 @@
+// Host-checkable logic of the decoding step's choices (verification of drafted tokens, eviction from a cache): keys,
+// sizes, workspace layout and addresses.  Compiled by hipcc for the library and by a plain host compiler for the tests.
+#ifndef NMS_DECODING_LOGIC_H
+#define NMS_DECODING_LOGIC_H
+
+#include <stddef.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "../../include/nms.h"
+#include "nms_pair.h"  // NMS_HD
+
+// ---- keys of the cache's order ----------------------------------------------------------------
+// A larger key stays longer; slots with equal keys stay in ascending order.  The bits are looked at, never compared as
+// floats, since device code is compiled without regard for NaN: sums that are not a number get the lowest key, and both
+// zeros the same one.  Protected rows lie above +infinity.
+#define NMS_CACHE_KEY_PROTECTED 0xffffffffu
+NMS_HD uint32_t nms_cache_key_bits(uint32_t u)
+{
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
+    if (u == 0x80000000u) u = 0u;
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+NMS_HD uint32_t nms_cache_key(float sum)
+{
+    uint32_t u;
+    memcpy(&u, &sum, sizeof u);
+    return nms_cache_key_bits(u);
+}
+
+// ---- sizes --------------------------------------------------------------------------------------
+NMS_HD int nms_moves_max(int n_max, int budget)
+{
+    const int behind = n_max > budget ? n_max - budget : 0;
+    return budget < behind ? budget : behind;
+}
+static inline size_t nms_decoding_align256(size_t v) { return (v + 255) & ~(size_t)255; }
+// Scratch of the whole path: the list of moves.
+static inline size_t nms_cache_scratch(int n_max, int frames, int budget)
+{
+    return nms_decoding_align256((size_t)frames * ((size_t)nms_moves_max(n_max, budget) + 1) * 2 * sizeof(int32_t));
+}
+
+// ---- addresses ----------------------------------------------------------------------------------
+// Byte offset of row (sequence, head, slot), or -1 when its page is none of the tensor's.
+NMS_HD long long nms_cache_row_offset(const nms_cache_tensor &t, const nms_cache_pages &pages, int sequence, int head, int slot)
+{
+    long long block = sequence;
+    if (pages.table != nullptr) {
+        block = pages.table[(long long)sequence * pages.table_stride + slot / pages.page_slots];
+        slot %= pages.page_slots;
+        if (block < 0 || block >= pages.pages) return -1;
+    }
+    return block * t.sequence_stride + head * t.head_stride + slot * t.slot_stride;
+}
+
+// Bytes that one lane moves at once: the widest power of two up to 16 that divides every address of the tensor's rows.
+static inline int nms_cache_piece(const nms_cache_tensor &t)
+{
+    const unsigned long long all = (unsigned long long)(uintptr_t)t.rows | (unsigned long long)t.row_bytes | (unsigned long long)t.sequence_stride |
+                                   (unsigned long long)t.head_stride | (unsigned long long)t.slot_stride | 16ull;
+    return (int)(all & (~all + 1));
+}
+
+#endif

@@ -12,9 +12,9 @@
 // 4 SGPRs and the 10 VALU instructions of the pair test.  The compare's lane mask IS the 64-bit
 // elimination word of (row r, column block): no cross-lane work is needed to form it.
 //
-// This file is the one translation unit of the library: the kernels live in kernels/*.h
-// (one file per step, included below inside the anonymous namespace), the launch logic and
-// the extern "C" entry points follow.
+// The kernels live in kernels/*.h (one file per step, included below inside the anonymous
+// namespace), the launch logic and the extern "C" entry points follow.  The decoding step's
+// choices are a translation unit of their own, decoding_kernels.hip.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -28,11 +28,14 @@
 #include "nms_pair.h"
 #include "nms_place.h"
 #include "nms_host_logic.h"
+#include "nms_launch.h"
 
 // Scratch of nms_run_static_batched: one copy per GPU, held from the moment the library is
 // loaded on it until the process ends.  In host code this name is only a handle for
 // hipGetSymbolAddress; the address the kernels use is static_scratch_on_current_device().
 static __device__ __align__(256) unsigned char scratch[NMS_STATIC_SCRATCH_BYTES];
+
+thread_local hipError_t nms_last_hip_error_of_thread = hipSuccess;
 
 namespace {
 
@@ -94,21 +97,6 @@ inline bool is_nan(float v)
     uint32_t b;
     memcpy(&b, &v, sizeof b);
     return (b & 0x7fffffffu) > 0x7f800000u;
-}
-
-thread_local hipError_t g_last_hip_error = hipSuccess;
-
-// The runtime's "last error" is per thread and sticky across libraries: an unrelated
-// earlier failure (for example a probe made by the host framework) would otherwise be
-// reported as ours.  begin_launch() discards it, launch_status() reads ours.
-inline void begin_launch() { (void)hipGetLastError(); }
-
-inline int launch_status()
-{
-    const hipError_t e = hipGetLastError();
-    if (e == hipSuccess) return NMS_OK;
-    g_last_hip_error = e;
-    return NMS_ERR_LAUNCH;
 }
 
 // The rank step by counting (nms_use_count_rank).
@@ -347,7 +335,7 @@ const char *nms_status_string(int status)
 
 int nms_version(void) { return NMS_VERSION; }
 
-const char *nms_last_launch_error(void) { return hipGetErrorString(g_last_hip_error); }
+const char *nms_last_launch_error(void) { return hipGetErrorString(nms_last_hip_error_of_thread); }
 
 int nms_padded_n(int n)
 {
@@ -641,7 +629,7 @@ static int run_routed(Route route, const float *boxes, const float *scores, cons
     auto mark = [&](int i) {
         if (!events || !events[i]) return true;
         const hipError_t e = hipEventRecord(static_cast<hipEvent_t>(events[i]), s);
-        if (e != hipSuccess) g_last_hip_error = e;
+        if (e != hipSuccess) nms_last_hip_error_of_thread = e;
         return e == hipSuccess;
     };
     if (!mark(0)) return NMS_ERR_LAUNCH;
@@ -1167,14 +1155,14 @@ static int static_scratch_on_current_device(void **out)
     static void *address[kMaxDevices] = {};
     int dev = -1;
     hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) { g_last_hip_error = e; return NMS_ERR_LAUNCH; }
+    if (e != hipSuccess) { nms_last_hip_error_of_thread = e; return NMS_ERR_LAUNCH; }
     if (dev < 0 || dev >= kMaxDevices) return NMS_ERR_INVALID_ARG;
     std::lock_guard<std::mutex> hold(lock);
     if (address[dev] == nullptr) {
         void *p = nullptr;
         e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch));
         if (e != hipSuccess || p == nullptr) {
-            g_last_hip_error = e != hipSuccess ? e : hipErrorInvalidSymbol;
+            nms_last_hip_error_of_thread = e != hipSuccess ? e : hipErrorInvalidSymbol;
             (void)hipGetLastError();
             return NMS_ERR_LAUNCH;
         }
