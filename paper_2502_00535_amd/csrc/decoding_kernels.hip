@@ -7,6 +7,8 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "nms_decoding_logic.h"
 #include "nms_launch.h"
 
@@ -38,11 +40,31 @@ inline int workspace_status(const void *workspace, size_t ws_bytes, size_t need)
     return workspace == nullptr || (uintptr_t)workspace % 256 != 0 || ws_bytes < need ? NMS_ERR_WORKSPACE : NMS_OK;
 }
 
-template <typename T>
-void verify_launch(const VerifyArgs &a, int sequences, hipStream_t stream)
+template <typename T, bool kDraft>
+int verify_launch(const VerifyArgs &a, int sequences, void *workspace, hipStream_t stream)
 {
-    if (a.draft != nullptr) verify_kernel<T, true><<<dim3(sequences), dim3(kVerifyThreads), 0, stream>>>(a);
-    else verify_kernel<T, false><<<dim3(sequences), dim3(kVerifyThreads), 0, stream>>>(a);
+    const int segments = nms_verify_segments(a.vocabulary);
+    const dim3 each(sequences), block(kVerifyThreads);
+    begin_launch();
+    if (nms_verify_in_one_launch(a.vocabulary, sequences)) {
+        verify_kernel<T, kDraft, false><<<each, block, 0, stream>>>(a, segments, VerifyScratch{nullptr, nullptr});
+        return launch_status();
+    }
+    char *room = static_cast<char *>(workspace);
+    const VerifyScratch scratch = {reinterpret_cast<double *>(room), reinterpret_cast<int2 *>(room + nms_verify_sums_bytes(a.vocabulary, sequences))};
+    const dim3 grid((segments + kVerifySumWaves - 1) / kVerifySumWaves, sequences);
+    verify_sums_kernel<T, kDraft><<<grid, dim3(kVerifySumWaves * 64), 0, stream>>>(a, segments, scratch);
+    const int st = launch_status();
+    if (st != NMS_OK) return st;
+    begin_launch();
+    verify_kernel<T, kDraft, true><<<each, block, 0, stream>>>(a, segments, scratch);
+    return launch_status();
+}
+
+template <typename T>
+int verify_launch(const VerifyArgs &a, int sequences, void *workspace, hipStream_t stream)
+{
+    return a.draft != nullptr ? verify_launch<T, true>(a, sequences, workspace, stream) : verify_launch<T, false>(a, sequences, workspace, stream);
 }
 
 int cache_sizes_status(int n_max, int heads, int sequences, int budget)
@@ -117,7 +139,7 @@ extern "C" {
 size_t nms_verify_workspace_bytes(int vocabulary, int sequences)
 {
     if (vocabulary < 1 || vocabulary > NMS_MAX_VOCABULARY || sequences < 0 || sequences > NMS_MAX_FRAMES) return 0;
-    return 0;
+    return nms_verify_scratch(vocabulary, sequences);
 }
 
 int nms_verify_batched(const void *target, long long target_stride, const void *draft, long long draft_stride, int type,
@@ -135,11 +157,10 @@ int nms_verify_batched(const void *target, long long target_stride, const void *
     const int st = workspace_status(workspace, ws_bytes, nms_verify_workspace_bytes(vocabulary, sequences));
     if (st != NMS_OK) return st;
     const VerifyArgs a = {target, draft, target_stride, draft_stride, drafts, counts, uniforms, tokens_out, accepted_out, drafts_max, vocabulary};
-    begin_launch();
-    if (type == NMS_TYPE_F32) verify_launch<float>(a, sequences, static_cast<hipStream_t>(stream));
-    else if (type == NMS_TYPE_F16) verify_launch<_Float16>(a, sequences, static_cast<hipStream_t>(stream));
-    else verify_launch<bf16_bits>(a, sequences, static_cast<hipStream_t>(stream));
-    return launch_status();
+    hipStream_t on = static_cast<hipStream_t>(stream);
+    if (type == NMS_TYPE_F32) return verify_launch<float>(a, sequences, workspace, on);
+    if (type == NMS_TYPE_F16) return verify_launch<_Float16>(a, sequences, workspace, on);
+    return verify_launch<bf16_bits>(a, sequences, workspace, on);
 }
 
 int nms_cache_moves_max(int n_max, int budget)

@@ -41,6 +41,28 @@ static inline size_t nms_cache_scratch(int n_max, int frames, int budget)
     return nms_decoding_align256((size_t)frames * ((size_t)nms_moves_max(n_max, budget) + 1) * 2 * sizeof(int32_t));
 }
 
+// ---- verification: the cut of a row, and the route -------------------------------------------
+#define NMS_VERIFY_SEGMENT 2048
+NMS_HD int nms_verify_segments(int vocabulary) { return (vocabulary + NMS_VERIFY_SEGMENT - 1) / NMS_VERIFY_SEGMENT; }
+// One launch with a workgroup per sequence where the row is short for sixteen wavefronts or the sequences fill the compute units, else the
+// segments' sums over the whole chip and a second launch.  Whole call, us, one launch / two (target and draft in f32; bf16): 1 x 8000 6.9 / 8.7, 6.6 / 8.6;
+// 1 x 40,000 9.5 / 9.9, 8.8 / 9.2; 1 x 50,000 11.3 / 9.5, 11.0 / 9.1; 64 x 50,000 12.0 / 11.5, 11.5 / 10.2; 128 x 50,000 14.1 / 15.9, 11.9 / 12.3;
+// 128 x 100,000 20.0 / 22.1, 17.1 / 17.4; 256 x 131,000 40.3 / 43.3, 25.1 / 28.0.
+static inline bool nms_verify_in_one_launch(int vocabulary, int sequences)
+{
+    return nms_verify_segments(vocabulary) <= 20 || sequences >= 128;
+}
+// Scratch of the route of two launches: the segments' sums, then what was accepted.
+static inline size_t nms_verify_sums_bytes(int vocabulary, int sequences)
+{
+    return nms_decoding_align256((size_t)sequences * (size_t)nms_verify_segments(vocabulary) * sizeof(double));
+}
+static inline size_t nms_verify_scratch(int vocabulary, int sequences)
+{
+    if (nms_verify_in_one_launch(vocabulary, sequences)) return 0;
+    return nms_verify_sums_bytes(vocabulary, sequences) + nms_decoding_align256((size_t)sequences * 2 * sizeof(int32_t));
+}
+
 // ---- addresses ----------------------------------------------------------------------------------
 // Byte offset of row (sequence, head, slot), or -1 when its page is none of the tensor's.
 NMS_HD long long nms_cache_row_offset(const nms_cache_tensor &t, const nms_cache_pages &pages, int sequence, int head, int slot)

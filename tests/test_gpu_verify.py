@@ -89,6 +89,28 @@ def test_a_token_does_not_depend_on_the_batch(nms):
     assert np.array_equal(t, tokens[:40]) and np.array_equal(a, accepted[:40])
 
 
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_a_long_row_in_large_and_small_batches(nms, with_draft):
+    """One launch for the large batch, two for the small one: the same tokens, and those of the definition."""
+    target, draft, drafts, u = inputs(4, 1, 60001, "f16", with_draft, 31)
+    few = agree(nms, target, draft, drafts, None, u)
+    many = [None if x is None else x.repeat(33, *[1] * (x.dim() - 1)) for x in (target, draft, drafts, u)]
+    tokens, accepted = call(nms, many[0], many[1], many[2], None, many[3])
+    assert np.array_equal(tokens, np.tile(few[0], (33, 1))) and np.array_equal(accepted, np.tile(few[1], 33))
+
+
+def test_nothing_left_of_the_difference_in_a_long_row(nms):
+    """The target's row in the difference's place, on the route of two launches."""
+    target = torch.zeros((2, 2, 100000))
+    target[:, :, [40000, 99999]] = 0.5
+    draft = torch.full((2, 1, 100000), 1.0)
+    tokens, accepted = agree(nms, target, draft, np.array([[7], [8]]), None, np.array([[0.0, 0.4], [0.9, 0.6]]))
+    assert accepted.tolist() == [0, 0] and tokens[:, 0].tolist() == [40000, 99999]
+    target[:, 0] = float("nan")
+    tokens, accepted = agree(nms, target, draft, np.array([[7], [8]]), [1, 0], np.array([[0.0, 0.4], [0.9, 0.6]]))
+    assert tokens.tolist() == [[-1, -1], [-1, -1]]
+
+
 @pytest.mark.parametrize("v", [64, 1024, 4096, 65536])
 def test_borders_between_equal_entries(nms, v):
     """Entries 1 / V, V a power of two: every sum is exact, and u = j / V lies on the border, where entry j begins."""
