@@ -27,8 +27,8 @@ __device__ __forceinline__ int frame_count(const int32_t *counts, int s, int n_m
 }
 
 #include "kernels/verify.h"
-#include "kernels/cache_keep.h"
 #include "kernels/cache_move.h"
+#include "kernels/cache_keep.h"
 
 // ----------------------------------------------------------------------------- host side
 
@@ -93,43 +93,92 @@ int tensors_status(const nms_cache_tensor *tensors, int n_tensors, const nms_cac
     return (long long)pages->table_stride * pages->page_slots < n_max ? NMS_ERR_INVALID_ARG : NMS_OK;
 }
 
-int add_launch(const CacheArgs &a, const nms_cache_weights *w, int frames, hipStream_t stream)
+WeightArgs weight_args(const nms_cache_weights *w)
 {
-    if (w == nullptr || w->group == 0 || w->tokens == 0 || w->columns == 0) return NMS_OK;
-    const WeightArgs args = {w->weights, w->row_stride, w->valid_tokens, w->group, w->tokens, w->columns};
-    const int columns = w->columns < a.n_max ? w->columns : a.n_max;
-    const dim3 grid((columns + 255) / 256, frames), block(256);
+    if (w == nullptr || w->group == 0 || w->tokens == 0 || w->columns == 0) return {};
+    return {w->weights, w->row_stride, w->valid_tokens, w->group, w->tokens, w->columns};
+}
+
+int add_launch(const CacheArgs &a, const WeightArgs &w, int type, int frames, hipStream_t stream)
+{
+    const int columns = w.columns < a.n_max ? w.columns : a.n_max;
+    const dim3 grid((columns + 255) / 256, frames), block(kAddWaves * 64);
     begin_launch();
-    if (w->type == NMS_TYPE_F32) cache_add_kernel<float><<<grid, block, 0, stream>>>(a, args);
-    else if (w->type == NMS_TYPE_F16) cache_add_kernel<_Float16><<<grid, block, 0, stream>>>(a, args);
-    else cache_add_kernel<bf16_bits><<<grid, block, 0, stream>>>(a, args);
+    if (type == NMS_TYPE_F32) cache_add_kernel<float><<<grid, block, 0, stream>>>(a, w);
+    else if (type == NMS_TYPE_F16) cache_add_kernel<_Float16><<<grid, block, 0, stream>>>(a, w);
+    else cache_add_kernel<bf16_bits><<<grid, block, 0, stream>>>(a, w);
     return launch_status();
 }
 
-int keep_launch(const CacheArgs &a, const nms_cache_weights *w, int frames, hipStream_t stream)
+template <int kVecs>
+int keep_launch(const CacheArgs &a, const WeightArgs &w, int type, const MoveArgs &m, int frames, hipStream_t stream)
 {
-    const int st = add_launch(a, w, frames, stream);
-    if (st != NMS_OK) return st;
+    const dim3 grid(frames), block((a.n_max + 256 * kVecs - 1) / (256 * kVecs) * 64);
+    const size_t lds = (size_t)a.moves_max * sizeof(uint16_t);
     begin_launch();
-    cache_keep_kernel<<<dim3(frames), dim3(kKeepThreads), 0, stream>>>(a);
+    if constexpr (kVecs <= 4) {
+        if (w.weights != nullptr) {
+            if (type == NMS_TYPE_F32) cache_keep_kernel<kVecs, float><<<grid, block, lds, stream>>>(a, w, m);
+            else if (type == NMS_TYPE_F16) cache_keep_kernel<kVecs, _Float16><<<grid, block, lds, stream>>>(a, w, m);
+            else cache_keep_kernel<kVecs, bf16_bits><<<grid, block, lds, stream>>>(a, w, m);
+            return launch_status();
+        }
+    }
+    cache_keep_kernel<kVecs, void><<<grid, block, lds, stream>>>(a, w, m);
     return launch_status();
 }
 
-int move_launch(const int32_t *moves, int n_max, int heads, int frames, int budget, const nms_cache_tensor *tensors, int n_tensors,
-                const nms_cache_pages *pages, hipStream_t stream)
+MoveArgs move_args(const int32_t *moves, int n_max, int heads, int budget, const nms_cache_tensor *tensors, int n_tensors,
+                   const nms_cache_pages *pages)
 {
     MoveArgs m = {};
     m.moves = moves, m.n_max = n_max, m.heads = heads, m.budget = budget, m.moves_max = nms_moves_max(n_max, budget), m.n_tensors = n_tensors;
-    if (m.moves_max == 0 || n_tensors == 0) return NMS_OK;
     if (pages != nullptr) m.pages = *pages;
     for (int i = 0; i < n_tensors; ++i) {
         m.tensors[i].t = tensors[i];
         m.tensors[i].piece = nms_cache_piece(tensors[i]);
         m.tensors[i].pieces = (int)(tensors[i].row_bytes / m.tensors[i].piece);
     }
+    return m;
+}
+
+int move_launch(const MoveArgs &m, int frames, hipStream_t stream)
+{
+    if (m.moves_max == 0 || m.n_tensors == 0) return NMS_OK;
     begin_launch();
     cache_move_kernel<<<dim3((m.moves_max + kMoveRows - 1) / kMoveRows, frames), dim3(256), 0, stream>>>(m);
     return launch_status();
+}
+
+// The keep vector and the moves; rows of `m` move in the same launch where there are few, by one of their own otherwise.
+int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const MoveArgs &m, int frames, hipStream_t stream)
+{
+    WeightArgs w = weight_args(weights);
+    const int type = weights != nullptr ? weights->type : 0;
+    if (w.weights != nullptr && !nms_cache_add_with_keep(a.n_max, w.group * (long long)w.tokens)) {
+        const int st = add_launch(a, w, type, frames, stream);
+        if (st != NMS_OK) return st;
+        w = {};
+    }
+    if (a.n_max > kKeepMaxWaves * 256 * 16) {
+        begin_launch();
+        cache_keep_long_kernel<<<dim3(frames), dim3(kKeepThreads), 0, stream>>>(a);
+        const int st = launch_status();
+        return st != NMS_OK ? st : move_launch(m, frames, stream);
+    }
+    const bool few = a.moves_max <= kFewCandidates;
+    CacheArgs b = a;
+    if (few && a.move_sums) b.moves = nullptr;  // the list stays in LDS
+    const MoveArgs none = {}, &now = few ? m : none;
+    int st;
+    switch (nms_cache_vecs(a.n_max)) {
+    case 1: st = keep_launch<1>(b, w, type, now, frames, stream); break;
+    case 2: st = keep_launch<2>(b, w, type, now, frames, stream); break;
+    case 4: st = keep_launch<4>(b, w, type, now, frames, stream); break;
+    case 8: st = keep_launch<8>(b, w, type, now, frames, stream); break;
+    default: st = keep_launch<16>(b, w, type, now, frames, stream); break;
+    }
+    return st != NMS_OK || few ? st : move_launch(m, frames, stream);
 }
 
 }  // namespace
@@ -190,7 +239,7 @@ int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t 
     if (st != NMS_OK) return st;
     const CacheArgs a = {sums, const_cast<int32_t *>(positions), counts, lengths, keep_out, kept_out, moves_out, n_max, heads, budget, first, recent,
                          nms_moves_max(n_max, budget), false};
-    return keep_launch(a, weights, heads * sequences, static_cast<hipStream_t>(stream));
+    return keep_and_move(a, weights, MoveArgs{}, heads * sequences, static_cast<hipStream_t>(stream));
 }
 
 int nms_cache_move_batched(const int32_t *moves, int n_max, int heads, int sequences, int budget, const nms_cache_tensor *tensors,
@@ -202,7 +251,7 @@ int nms_cache_move_batched(const int32_t *moves, int n_max, int heads, int seque
     if (st != NMS_OK) return st;
     if (n_max == 0 || heads == 0 || sequences == 0 || n_tensors == 0) return NMS_OK;
     if (moves == nullptr) return NMS_ERR_INVALID_ARG;
-    return move_launch(moves, n_max, heads, heads * sequences, budget, tensors, n_tensors, pages, static_cast<hipStream_t>(stream));
+    return move_launch(move_args(moves, n_max, heads, budget, tensors, n_tensors, pages), heads * sequences, static_cast<hipStream_t>(stream));
 }
 
 int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *counts, const int32_t *lengths, int n_max,
@@ -225,9 +274,7 @@ int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *coun
     int32_t *moves = static_cast<int32_t *>(workspace);
     const CacheArgs a = {sums, positions, counts, lengths, keep_out, kept_out, moves, n_max, heads, budget, first, recent,
                          nms_moves_max(n_max, budget), true};
-    st = keep_launch(a, weights, frames, static_cast<hipStream_t>(stream));
-    if (st != NMS_OK) return st;
-    return move_launch(moves, n_max, heads, frames, budget, tensors, n_tensors, pages, static_cast<hipStream_t>(stream));
+    return keep_and_move(a, weights, move_args(moves, n_max, heads, budget, tensors, n_tensors, pages), frames, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

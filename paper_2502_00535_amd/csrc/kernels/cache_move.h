@@ -21,23 +21,20 @@ __device__ __forceinline__ void move_piece(char *to, const char *from, int j)
     reinterpret_cast<P *>(to)[j] = reinterpret_cast<const P *>(from)[j];
 }
 
-// A row's source lies at or beyond slot k and its target below, so no row is both and all moves are independent.
-constexpr int kMoveRows = 32;
-__global__ void __launch_bounds__(256) cache_move_kernel(MoveArgs a)
+// Rows r = 0 .. rows - 1 of a frame by `threads` threads; move(r) names (to, from).  A row's source lies at or beyond slot `budget` and its target
+// below, so no row is both and all moves are independent.
+template <typename Move>
+__device__ __forceinline__ void move_rows(const MoveArgs &a, int frame, int rows, int threads, Move &&move)
 {
-    const int frame = blockIdx.y, sequence = frame / a.heads, head = frame % a.heads;
-    const int32_t *list = a.moves + (long long)frame * (a.moves_max + 1) * 2;
-    const int total = min(list[0], a.moves_max);
-    const int begin = blockIdx.x * kMoveRows, rows = min(total - begin, kMoveRows);
-    if (rows <= 0) return;
+    const int sequence = frame / a.heads, head = frame % a.heads;
     for (int which = 0; which < a.n_tensors; ++which) {
         const MoveTensor &m = a.tensors[which];
-        for (int w = threadIdx.x; w < rows * m.pieces; w += 256) {
+        for (int w = threadIdx.x; w < rows * m.pieces; w += threads) {
             const int r = w / m.pieces, j = w - r * m.pieces;
-            const int to = list[2 + 2 * (begin + r)], from = list[3 + 2 * (begin + r)];
-            if (to < 0 || to >= a.budget || from < a.budget || from >= a.n_max) continue;
-            const long long t = nms_cache_row_offset(m.t, a.pages, sequence, head, to);
-            const long long s = nms_cache_row_offset(m.t, a.pages, sequence, head, from);
+            const int2 pair = move(r);
+            if (pair.x < 0 || pair.x >= a.budget || pair.y < a.budget || pair.y >= a.n_max) continue;
+            const long long t = nms_cache_row_offset(m.t, a.pages, sequence, head, pair.x);
+            const long long s = nms_cache_row_offset(m.t, a.pages, sequence, head, pair.y);
             if (t < 0 || s < 0) continue;
             char *rows_at = static_cast<char *>(m.t.rows);
             if (m.piece == 16) move_piece<uint4>(rows_at + t, rows_at + s, j);
@@ -47,4 +44,13 @@ __global__ void __launch_bounds__(256) cache_move_kernel(MoveArgs a)
             else move_piece<uint8_t>(rows_at + t, rows_at + s, j);
         }
     }
+}
+
+constexpr int kMoveRows = 32;
+__global__ void __launch_bounds__(256) cache_move_kernel(MoveArgs a)
+{
+    const int frame = blockIdx.y;
+    const int2 *list = reinterpret_cast<const int2 *>(a.moves) + (long long)frame * (a.moves_max + 1);
+    const int begin = blockIdx.x * kMoveRows, rows = min(min(list[0].x, a.moves_max) - begin, kMoveRows);
+    if (rows > 0) move_rows(a, frame, rows, 256, [&](int r) { return list[1 + begin + r]; });
 }

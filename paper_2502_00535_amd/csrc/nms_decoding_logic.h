@@ -41,6 +41,17 @@ static inline size_t nms_cache_scratch(int n_max, int frames, int budget)
     return nms_decoding_align256((size_t)frames * ((size_t)nms_moves_max(n_max, budget) + 1) * 2 * sizeof(int32_t));
 }
 
+// ---- eviction: the route ------------------------------------------------------------------------
+// Vectors of four slots to a lane: a frame is one workgroup of at most sixteen wavefronts.
+static inline int nms_cache_vecs(int n_max)
+{
+    int vecs = n_max <= 1024 ? 1 : 2;
+    while (n_max > 16 * 256 * vecs) vecs *= 2;
+    return vecs;
+}
+// The weights are added by the launch that finds the rows that stay where there are few query rows, by one of its own otherwise.
+static inline bool nms_cache_add_with_keep(int n_max, long long rows) { return rows <= 32 && nms_cache_vecs(n_max) <= 4; }
+
 // ---- verification: the cut of a row, and the route -------------------------------------------
 #define NMS_VERIFY_SEGMENT 2048
 NMS_HD int nms_verify_segments(int vocabulary) { return (vocabulary + NMS_VERIFY_SEGMENT - 1) / NMS_VERIFY_SEGMENT; }

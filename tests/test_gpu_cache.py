@@ -133,7 +133,7 @@ def attention(s, h, group, tokens, columns, kind, seed):
 
 
 SIZES = [(1, 1, 1, 1), (1, 1, 1, 0), (2, 1, 2, 1), (1, 3, 63, 20), (2, 2, 64, 64), (1, 2, 65, 64), (1, 1, 65, 200), (3, 2, 127, 1), (2, 3, 1000, 999), (1, 8, 1025, 1024),
-         (2, 2, 1024, 0), (1, 2, 2047, 512), (2, 1, 4097, 4000), (2, 2, 5003, 1501), (1, 2, 9001, 100), (1, 1, 20011, 19000), (1, 2, 33333, 4096), (1, 1, 66001, 8192), (300, 1, 200, 150)]
+         (2, 2, 1024, 0), (1, 2, 2047, 512), (2, 1, 4097, 4000), (2, 2, 5003, 1501), (1, 2, 9001, 100), (1, 1, 20011, 19000), (1, 2, 33333, 4096), (1, 1, 65536, 32768), (1, 1, 66001, 8192), (1, 2, 1025, 961), (2, 2, 8192, 8128), (2, 1, 16385, 16000), (300, 1, 200, 150)]
 
 
 @pytest.mark.parametrize("s,h,n,budget", SIZES)
