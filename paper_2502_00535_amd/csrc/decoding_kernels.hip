@@ -166,7 +166,7 @@ int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const Mo
         const int st = launch_status();
         return st != NMS_OK ? st : move_launch(m, frames, stream);
     }
-    const bool few = a.moves_max <= kFewCandidates;
+    const bool few = a.moves_max <= kFew;
     CacheArgs b = a;
     if (few && a.move_sums) b.moves = nullptr;  // the list stays in LDS
     const MoveArgs none = {}, &now = few ? m : none;

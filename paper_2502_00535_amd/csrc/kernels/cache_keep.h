@@ -110,14 +110,13 @@ __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, 
     store_four(sums, i, n, s);
 }
 
-// ---- the rows that stay: one workgroup per frame, all of its slots in registers
+// ---- the rows that stay: one workgroup per frame, the keys of all its slots in registers
 
 // A lane has kVecs times four neighbouring slots, a wavefront 256 * kVecs neighbouring ones, so that the rank of a slot among others is a
 // count over the wavefronts before, the vectors before, the lanes before and the lane's own.
 constexpr int kKeepMaxWaves = 16;
-constexpr int kKeepBinsPerThread = 2;
-constexpr int kKeepBins = kKeepMaxWaves * 64 * kKeepBinsPerThread;
-constexpr int kFewCandidates = 64;
+constexpr int kKeepBins = kKeepMaxWaves * 64 * 2;  // two to a thread
+constexpr int kFew = 64;                           // candidates that are compared one with another; moves that need no list in memory
 
 // Keys of slots that hold a row are at least 1, so that 0 can stand for those that hold none.
 __device__ __forceinline__ uint32_t live_key(float sum, bool protect)
@@ -125,133 +124,84 @@ __device__ __forceinline__ uint32_t live_key(float sum, bool protect)
     return protect ? NMS_CACHE_KEY_PROTECTED : nms_cache_key_bits(__float_as_uint(sum)) + 1u;
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+// Over the 64 lanes of a wavefront, all of them active: the largest number (in every lane), and running counts.
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_fold(uint32_t x, Op &&op)
 {
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
-    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
-}
-__device__ __forceinline__ uint32_t wave_running_count(uint32_t x)  // inclusive, over the lanes
-{
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
+    x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));   // row_shr:1
+    x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));   // row_shr:2
+    x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));   // row_shr:4
+    x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));   // row_shr:8
+    x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));  // row_bcast:15 into rows 1, 3
+    x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));  // row_bcast:31 into rows 2, 3
     return x;
 }
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) { return of_lane(wave_fold(x, [](uint32_t p, uint32_t q) { return max(p, q); }), 63); }
+__device__ __forceinline__ uint32_t wave_running_count(uint32_t x) { return wave_fold(x, [](uint32_t p, uint32_t q) { return p + q; }); }
 
 struct KeepRoom {
     uint32_t bins[kKeepBins];
     uint32_t wave_a[kKeepMaxWaves], wave_b[kKeepMaxWaves], wave_c[kKeepMaxWaves];
-    uint32_t found[3];                        // bin, how many lie beyond it, how many in it
-    uint32_t few, few_keys[kFewCandidates], few_slots[kFewCandidates];
+    uint32_t found[3];             // bin, how many lie beyond it, how many in it
+    uint32_t few, few_keys[kFew];
+    uint16_t from[kFew];
 };
 
-// Where the order is cut: a row stays if its key is larger, or the same and its slot not beyond the last one.
+// Where the best `need` of the `left` keys between lo and hi end (0 < need <= left): at the least that stays, and how many keys equal to it are
+// wanted and there.
 struct Cut {
-    uint32_t key;
-    int last;
+    uint32_t key, wanted, there;
 };
 
-// The cut behind the best k of n rows, 0 < k < n.  Keys are counted in bins between the smallest and the largest, the bin in which the k-th
-// lies is cut into bins again, until it has few rows (they are compared one with another) or a single key; then the same by slots.  Counting
-// costs an atomic addition in LDS per row and round; sums of attention weights spread over dozens of binary orders, so that one or two rounds do.  Lanes of a
-// wavefront that fall into the first one's bin are added as one, or rows with equal sums would queue up there.
-template <int kVecs, typename Key>
-__device__ Cut find_cut(KeepRoom &room, int k, Key &&key, int base_slot, int wave, int lane)
+// Keys are counted in bins between lo and hi, the bin in which the need-th lies is cut into bins again, until few keys are left (which are compared
+// one with another), or one, or all that are left are wanted.  Counting costs an atomic addition in LDS per key and round; sums of attention weights
+// spread over dozens of binary orders, so that a round or two do.  Lanes that fall into the bin of the first one are added as one: rows with equal
+// sums would queue up there.
+template <int kVecs>
+__device__ __forceinline__ Cut find_cut(KeepRoom &room, const uint32_t (&key)[kVecs * 4], uint32_t lo, uint32_t hi, uint32_t need, uint32_t left,
+                                        int wave, int lane)
 {
-    const int waves = blockDim.x >> 6, bins = blockDim.x * kKeepBinsPerThread;
-    uint32_t largest = 0, smallest = 0, rows = 0, guarded = 0;  // smallest: of the complement
-#pragma unroll
-    for (int e = 0; e < kVecs * 4; ++e) {
-        const uint32_t u = key(e);
-        const bool row = u != 0u, protect = u == NMS_CACHE_KEY_PROTECTED;
-        guarded += __popcll(__ballot(protect));
-        rows += __popcll(__ballot(row && !protect));
-        largest = max(largest, protect ? 0u : u);
-        smallest = max(smallest, row && !protect ? ~u : 0u);
-    }
-    largest = wave_max(largest);
-    smallest = wave_max(smallest);
-    if (lane == 0) room.wave_a[wave] = largest, room.wave_b[wave] = smallest, room.wave_c[wave] = rows, room.bins[wave] = guarded;
-    __syncthreads();
-    rows = guarded = 0;
-    for (int i = 0; i < waves; ++i) {
-        largest = max(largest, room.wave_a[i]);
-        smallest = max(smallest, room.wave_b[i]);
-        rows += room.wave_c[i];
-        guarded += room.bins[i];
-    }
-    __syncthreads();
-    uint32_t lo = ~smallest, hi = largest, need = (uint32_t)k - guarded, left = rows;
-    bool by_slot = false;       // the second stage: among rows of one key (lo == hi == cut.key), by the complement of their slots
-    Cut cut = {0u, 0x7fffffff};
-    if ((uint32_t)k <= guarded) {  // more protected rows than may stay
-        if ((uint32_t)k == guarded) return {NMS_CACHE_KEY_PROTECTED - 1u, -1};
-        lo = hi = NMS_CACHE_KEY_PROTECTED, need = (uint32_t)k, left = guarded;
-    }
+    const int log_bins = 31 - __builtin_clz(blockDim.x * 2);
     for (;;) {
-        if (left == need) {  // all of them: the cut lies below
-            if (by_slot) return {cut.key, (int)~lo};
-            return {lo, 0x7fffffff};
-        }
-        if (!by_slot && lo == hi) {
-            by_slot = true;
-            cut.key = lo;
-            lo = ~(uint32_t)(waves * 256 * kVecs - 1), hi = ~0u;  // complements of the frame's slots
-        }
-        auto value = [&](int e) { return by_slot ? ~(uint32_t)(base_slot + (e >> 2) * 256 + (e & 3)) : key(e); };
-        auto among = [&](int e, uint32_t v) { return v >= lo && v <= hi && (!by_slot || key(e) == cut.key); };
-        if (left <= kFewCandidates) {
+        if (left == need) return {lo, 0u, 0u};    // all that are left: whatever lies at or beyond lo
+        if (lo == hi) return {lo, need, left};
+        const uint32_t range = hi - lo;
+        if (left <= (uint32_t)kFew) {
             if (threadIdx.x == 0) room.few = 0;
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < kVecs * 4; ++e) {
-                const uint32_t v = value(e);
-                if (among(e, v)) {
-                    const uint32_t at = atomicAdd(&room.few, 1u);
-                    if (at < (uint32_t)kFewCandidates) {
-                        room.few_keys[at] = key(e);
-                        room.few_slots[at] = (uint32_t)(base_slot + (e >> 2) * 256 + (e & 3));
-                    }
-                }
-            }
+            for (int e = 0; e < kVecs * 4; ++e)
+                if (key[e] - lo <= range) room.few_keys[atomicAdd(&room.few, 1u) & (kFew - 1)] = key[e];
             __syncthreads();
-            const uint32_t mine = lane < (int)left ? room.few_keys[lane] : 0u, slot = lane < (int)left ? room.few_slots[lane] : ~0u;
-            uint32_t rank = 0;
+            const bool there = lane < (int)left;
+            const uint32_t mine = there ? room.few_keys[lane] : 0u;
+            uint32_t larger = 0, equal = 0;
             for (int i = 0; i < (int)left; ++i) {
-                const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, i), at = (uint32_t)__builtin_amdgcn_readlane((int)slot, i);
-                rank += other > mine || (other == mine && at < slot);
+                const uint32_t other = of_lane(mine, i);
+                larger += other > mine;
+                equal += other == mine;
             }
-            const int which = __builtin_ctzll(__ballot(lane < (int)left && rank == need - 1) | (1ull << 63));
-            return {(uint32_t)__builtin_amdgcn_readlane((int)mine, which), __builtin_amdgcn_readlane((int)slot, which)};
+            const unsigned long long at = __ballot(there && larger < need && need <= larger + equal);
+            const int which = __builtin_ctzll(at | (1ull << 63));
+            return {of_lane(mine, which), need - of_lane(larger, which), of_lane(equal, which)};
         }
-        const uint32_t range = hi - lo;
-        int shift = 0;
-        while ((range >> shift) >= (uint32_t)bins) ++shift;
-#pragma unroll
-        for (int i = 0; i < kKeepBinsPerThread; ++i) room.bins[i * blockDim.x + threadIdx.x] = 0;
+        const int bits = 32 - __builtin_clz(range), shift = bits > log_bins ? bits - log_bins : 0;
+        room.bins[threadIdx.x] = 0;
+        room.bins[blockDim.x + threadIdx.x] = 0;
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < kVecs * 4; ++e) {
-            const uint32_t v = value(e), bin = (v - lo) >> shift;
-            const bool in = among(e, v);
-            const unsigned long long who = __ballot(in);
-            if (who == 0) continue;
-            const int leader = __builtin_ctzll(who);
-            const bool same = in && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, leader);
-            const int many = __popcll(__ballot(same));
-            if (lane == leader) atomicAdd(&room.bins[bin], (uint32_t)many);
-            else if (in && !same) atomicAdd(&room.bins[bin], 1u);
+            const uint32_t v = key[e] - lo, bin = v >> shift;
+            const unsigned long long in = __ballot(v <= range);
+            if (in != 0) {
+                const unsigned long long same = __ballot(bin == of_lane(bin, __builtin_ctzll(in))) & in;
+                const unsigned long long leader = same & (0ull - same);
+                if (((in & ~same) | leader) >> lane & 1) atomicAdd(&room.bins[bin], (leader >> lane & 1) != 0 ? (uint32_t)__popcll(same) : 1u);
+            }
         }
         __syncthreads();
-        // thread t has bins 2 t and 2 t + 1; how many rows lie in larger bins
+        // thread t has bins 2 t and 2 t + 1; how many keys lie in larger bins
         const uint32_t b0 = room.bins[2 * threadIdx.x], b1 = room.bins[2 * threadIdx.x + 1], own = b0 + b1;
         const uint32_t upto = wave_running_count(own);
         if (lane == 63) room.wave_a[wave] = upto;
@@ -266,10 +216,9 @@ __device__ Cut find_cut(KeepRoom &room, int k, Key &&key, int base_slot, int wav
             room.found[2] = upper ? b1 : b0;
         }
         __syncthreads();
-        const uint32_t bin = room.found[0];
         need -= room.found[1];
         left = room.found[2];
-        lo += bin << shift;
+        lo += room.found[0] << shift;
         const uint32_t top = lo + ((1u << shift) - 1u);
         hi = top < lo || top > hi ? hi : top;
     }
@@ -278,57 +227,118 @@ __device__ Cut find_cut(KeepRoom &room, int k, Key &&key, int base_slot, int wav
 template <int kVecs, typename W>
 __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArgs a, WeightArgs w, MoveArgs m)
 {
+    constexpr int kEach = kVecs * 4;
+    constexpr bool kWeights = !std::is_same<W, void>::value;
     __shared__ KeepRoom room;
     extern __shared__ uint16_t targets[];  // free slots in their order, moves_max of them
     const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int n = slots_of(a, sequence), k = min(n, a.budget);
     const long long base = (long long)frame * a.n_max;
     const int length = a.lengths != nullptr ? a.lengths[sequence] : n;
-    const int base_slot = wave * (256 * kVecs) + lane * 4;  // of element e: base_slot + (e >> 2) * 256 + (e & 3)
-    float sum[kVecs * 4];
-    unsigned long long guard = 0;
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-        const int i = base_slot + v * 256;
-        const Four<float> s = load_four(a.sums + base, i, n);
-        Four<int32_t> p = {{i, i + 1, i + 2, i + 3}};
-        if (a.positions != nullptr) p = load_four(a.positions + base, i, n);
+    const int base_slot = wave * (256 * kVecs) + lane * 4;
+    auto slot_of = [&](int e) { return base_slot + (e >> 2) * 256 + (e & 3); };
+    const bool whole = (wave + 1) * (256 * kVecs) <= n;  // of the wavefront: every slot holds a row
+    uint32_t key[kEach], largest = 0, smallest = 0, guarded = 0;  // smallest: as its complement; both without the protected rows
+    auto take = [&](int v, const Four<float> &s, const Four<int32_t> &p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            sum[v * 4 + j] = s.v[j];
             const bool protect = p.v[j] < a.first || (long long)p.v[j] >= (long long)length - a.recent;
-            guard |= (unsigned long long)protect << (v * 4 + j);
+            const uint32_t u = live_key(s.v[j], protect);
+            const bool there = whole || base_slot + v * 256 + j < n;
+            key[v * 4 + j] = there ? u : 0u;
+            largest = max(largest, there && !protect ? u : 0u);
+            smallest = max(smallest, there && !protect ? ~u : 0u);
+            guarded += there && protect;
         }
-    }
-    if constexpr (!std::is_same<W, void>::value) {
+    };
+    auto places = [&](int v) {
+        const int i = base_slot + v * 256;
+        if (a.positions == nullptr) return Four<int32_t>{{i, i + 1, i + 2, i + 3}};
+        return whole ? *reinterpret_cast<const Four<int32_t> *>(a.positions + base + i) : load_four(a.positions + base, i, n);
+    };
+    auto sums_of = [&](int v) {
+        const int i = base_slot + v * 256;
+        return whole ? *reinterpret_cast<const Four<float> *>(a.sums + base + i) : load_four(a.sums + base, i, n);
+    };
+    if constexpr (kWeights) {
         const int columns = min(n, w.columns), tokens = valid_of(w, sequence);
         const W *row = static_cast<const W *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
-        double total[kVecs * 4];
+        Four<int32_t> p[kVecs];
+        Four<float> s[kVecs];
+        double total[kEach];
 #pragma unroll
-        for (int e = 0; e < kVecs * 4; ++e) total[e] = (double)sum[e];
+        for (int v = 0; v < kVecs; ++v) s[v] = sums_of(v);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) p[v] = places(v);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) total[e] = (double)s[e >> 2].v[e & 3];
+        const bool all = (wave + 1) * (256 * kVecs) <= columns;
         for (int g = 0; g < w.group; ++g)
-#pragma unroll 2
             for (int t = 0; t < tokens; ++t) {
                 const W *at = row + ((long long)g * w.tokens + t) * w.row_stride;
                 Four<W> x[kVecs];
 #pragma unroll
-                for (int v = 0; v < kVecs; ++v) x[v] = load_four(at, base_slot + v * 256, columns);
+                for (int v = 0; v < kVecs; ++v) {
+                    const int i = base_slot + v * 256;
+                    x[v] = all ? *reinterpret_cast<const Four<W> *>(at + i) : load_four(at, i, columns);
+                }
 #pragma unroll
-                for (int e = 0; e < kVecs * 4; ++e) total[e] += as_weight(x[e >> 2].v[e & 3]);
+                for (int e = 0; e < kEach; ++e) total[e] += as_weight(x[e >> 2].v[e & 3]);
             }
 #pragma unroll
-        for (int e = 0; e < kVecs * 4; ++e) sum[e] = (float)total[e];
-    }
-    auto slot_of = [&](int e) { return base_slot + (e >> 2) * 256 + (e & 3); };
-    auto key = [&](int e) { return slot_of(e) < n ? live_key(sum[e], guard >> e & 1) : 0u; };
-    Cut cut = {0u, -1};                                          // all rows stay
-    if (k == 0) cut.key = ~0u;                                   // none does
-    else if (k < n) cut = find_cut<kVecs>(room, k, key, base_slot, wave, lane);
-    unsigned long long stay = 0;
+        for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
-    for (int e = 0; e < kVecs * 4; ++e) {
-        const uint32_t u = key(e);
-        stay |= (unsigned long long)(u > cut.key || (u == cut.key && u != 0u && slot_of(e) <= cut.last)) << e;
+            for (int j = 0; j < 4; ++j) s[v].v[j] = (float)total[v * 4 + j];
+            store_four(a.sums + base, base_slot + v * 256, n, s[v]);
+            take(v, s[v], p[v]);
+        }
+    } else {
+        constexpr int kAtOnce = kVecs < 4 ? kVecs : 4;
+#pragma unroll
+        for (int v0 = 0; v0 < kVecs; v0 += kAtOnce) {
+            Four<int32_t> p[kAtOnce];
+            Four<float> s[kAtOnce];
+#pragma unroll
+            for (int v = 0; v < kAtOnce; ++v) s[v] = sums_of(v0 + v);
+#pragma unroll
+            for (int v = 0; v < kAtOnce; ++v) p[v] = places(v0 + v);
+#pragma unroll
+            for (int v = 0; v < kAtOnce; ++v) take(v0 + v, s[v], p[v]);
+        }
+    }
+    // which rows stay, a bit to an element
+    using Bits = typename std::conditional<(kEach > 32), unsigned long long, uint32_t>::type;
+    Bits stay = 0;
+    if (k == n) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] != 0u) << e;
+    } else if (k > 0) {
+        largest = wave_max(largest);
+        smallest = wave_max(smallest);
+        guarded = wave_running_count(guarded);
+        if (lane == 63) room.wave_a[wave] = largest, room.wave_b[wave] = smallest, room.wave_c[wave] = guarded;
+        __syncthreads();
+        guarded = 0;
+        for (int i = 0; i < waves; ++i) {
+            largest = max(largest, room.wave_a[i]);
+            smallest = max(smallest, room.wave_b[i]);
+            guarded += room.wave_c[i];
+        }
+        __syncthreads();
+        uint32_t lo = ~smallest, hi = largest, need = (uint32_t)k - guarded, left = (uint32_t)n - guarded;
+        if ((uint32_t)k <= guarded) lo = hi = NMS_CACHE_KEY_PROTECTED, need = (uint32_t)k, left = guarded;  // protected rows alone
+        Cut cut;
+        for (int stage = 0;; ++stage) {
+            cut = find_cut<kVecs>(room, key, lo, hi, need, left, wave, lane);
+            const bool ties = cut.wanted < cut.there;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] > cut.key || (key[e] == cut.key && !ties)) << e;
+            if (!ties) break;
+            // of the rows with that key the lowest slots: once more, with the complements of their slots for keys (no two are the same)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) key[e] = key[e] == cut.key ? ~(uint32_t)slot_of(e) : 0u;
+            lo = ~(uint32_t)(waves * 256 * kVecs - 1), hi = ~0u, need = cut.wanted, left = cut.there;
+        }
     }
     if (a.keep != nullptr) {
 #pragma unroll
@@ -340,82 +350,65 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         }
     }
     if (a.kept != nullptr && threadIdx.x == 0 && frame % a.heads == 0) a.kept[sequence] = k;
+    if (a.moves == nullptr && !a.move_sums) return;
     // moves: slots below k whose row goes are free, rows that stay beyond take them in order
-    unsigned long long is_free = 0, moves = 0;
-    uint32_t frees = 0, moved = 0;
-    if (a.moves_max > 0 && (a.moves != nullptr || a.move_sums)) {
+    Bits is_free = 0, moves = 0;
 #pragma unroll
-        for (int e = 0; e < kVecs * 4; ++e) {
-            const int i = slot_of(e);
-            const bool s = stay >> e & 1, f = i < k && !s, b = i >= k && s;
-            is_free |= (unsigned long long)f << e;
-            moves |= (unsigned long long)b << e;
-            frees += __popcll(__ballot(f));
-            moved += __popcll(__ballot(b));
-        }
+    for (int e = 0; e < kEach; ++e) {
+        const bool s = stay >> e & 1, low = slot_of(e) < k;
+        is_free |= (Bits)(low && !s) << e;
+        moves |= (Bits)(!low && s) << e;
     }
-    if (lane == 0) room.wave_b[wave] = frees, room.wave_c[wave] = moved;
+    const uint32_t counts = wave_running_count((uint32_t)__popcll(is_free) << 16 | (uint32_t)__popcll(moves));  // at most 4096 of each in a wavefront
+    if (lane == 63) room.wave_b[wave] = counts;
     __syncthreads();
     uint32_t to = 0, from = 0, total = 0;
     for (int i = 0; i < waves; ++i) {
-        to += i < wave ? room.wave_b[i] : 0;
-        from += i < wave ? room.wave_c[i] : 0;
-        total += room.wave_c[i];
+        const uint32_t c = room.wave_b[i];
+        to += i < wave ? c >> 16 : 0u;
+        from += i < wave ? c & 0xffffu : 0u;
+        total += c & 0xffffu;
     }
-    const unsigned long long before = (1ull << lane) - 1;
-    // ranks in order of slots: visit(e, rank) for each flagged element
-    auto ranked = [&](unsigned long long flags, uint32_t rank0, auto &&visit) {
+    // in order of slots: visit(element, its rank) for each of the flagged
+    auto ranked = [&](Bits flags, uint32_t rank0, auto &&visit) {
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
-            uint32_t rank = rank0, all = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned long long mask = __ballot(flags >> (v * 4 + j) & 1);
-                rank += __popcll(mask & before);
-                all += __popcll(mask);
-            }
+            const uint32_t own = (uint32_t)(flags >> (v * 4)) & 15u;
+            if (__ballot(own != 0) == 0) continue;
+            const uint32_t upto = wave_running_count(__popc(own));
+            uint32_t rank = rank0 + upto - __popc(own);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (flags >> (v * 4 + j) & 1) visit(v * 4 + j, rank++);
-            rank0 += all;
+                if (own >> j & 1) visit(v * 4 + j, rank++);
+            rank0 += of_lane(upto, 63);
         }
     };
-    if (frees > 0) ranked(is_free, to, [&](int e, uint32_t r) { targets[r] = (uint16_t)slot_of(e); });
+    ranked(is_free, to, [&](int e, uint32_t r) { targets[r] = (uint16_t)slot_of(e); });
     __syncthreads();
     int2 *list = a.moves != nullptr ? reinterpret_cast<int2 *>(a.moves) + (long long)frame * (a.moves_max + 1) : nullptr;
     if (list != nullptr && threadIdx.x == 0) list[0] = make_int2((int)total, 0);
-    if (moved > 0)
-        ranked(moves, from, [&](int e, uint32_t r) {
-            const int t = targets[r], i = slot_of(e);
-            if (list != nullptr) list[1 + r] = make_int2(t, i);
-            if (r < (uint32_t)kFewCandidates) room.few_slots[r] = (uint32_t)i;
-            if (a.move_sums) {
-                a.sums[base + t] = sum[e];
-                if (a.positions != nullptr) a.positions[base + t] = a.positions[base + i];
-            }
-        });
-    // sums as they are held now: added (with weights), moved, and none behind the rows that stay
-    if (a.move_sums || !std::is_same<W, void>::value) {
+    ranked(moves, from, [&](int e, uint32_t r) {
+        const int t = targets[r], i = slot_of(e);
+        if (list != nullptr) list[1 + r] = make_int2(t, i);
+        if (r < (uint32_t)kFew) room.from[r] = (uint16_t)i;
+        if (a.move_sums) {
+            a.sums[base + t] = a.sums[base + i];
+            if (a.positions != nullptr) a.positions[base + t] = a.positions[base + i];
+        }
+    });
+    if (!a.move_sums) return;
+    __syncthreads();
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-            const int i = base_slot + v * 256;
-            Four<float> s;
+    for (int v = 0; v < kVecs; ++v) {  // behind the rows that stay: no sums
+        const int i = base_slot + v * 256;
+        if (i >= k) store_four(a.sums + base, i, n, Four<float>{});
+        else if (i + 4 > k) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s.v[j] = a.move_sums && i + j >= k ? 0.0f : sum[v * 4 + j];
-            const bool none_free = !a.move_sums || (is_free >> (v * 4) & 15) == 0;
-            if (!std::is_same<W, void>::value || (i + 4 > k && i < n)) {
-                if (none_free) store_four(a.sums + base, i, n, s);
-                else
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (i + j < n && !(is_free >> (v * 4 + j) & 1)) a.sums[base + i + j] = s.v[j];
-            }
+            for (int j = 1; j < 4; ++j)
+                if (i + j >= k && i + j < n) a.sums[base + i + j] = 0.0f;
         }
     }
-    if (m.n_tensors > 0) {  // few rows to move: in the same launch
-        __syncthreads();
-        move_rows(m, frame, (int)total, (int)blockDim.x, [&](int r) { return make_int2(targets[r], (int)room.few_slots[r]); });
-    }
+    if (m.n_tensors > 0) move_rows(m, frame, (int)total, (int)blockDim.x, [&](int r) { return make_int2(targets[r], room.from[r]); });  // few rows: in this launch
 }
 
 constexpr int kKeepThreads = 1024;
