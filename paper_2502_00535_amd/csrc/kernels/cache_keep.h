@@ -156,8 +156,8 @@ struct Cut {
 
 // Keys are counted in bins between lo and hi, the bin in which the need-th lies is cut into bins again, until few keys are left (which are compared
 // one with another), or one, or all that are left are wanted.  Counting costs an atomic addition in LDS per key and round; sums of attention weights
-// spread over dozens of binary orders, so that a round or two do.  Lanes that fall into the bin of the first one are added as one: rows with equal
-// sums would queue up there.
+// spread over dozens of binary orders, so that a round or two do.  Where the lanes of a wavefront crowd into one bin (equal sums: they would queue up
+// there) they are added as one.
 template <int kVecs>
 __device__ __forceinline__ Cut find_cut(KeepRoom &room, const uint32_t (&key)[kVecs * 4], uint32_t lo, uint32_t hi, uint32_t need, uint32_t left,
                                         int wave, int lane)
@@ -191,13 +191,23 @@ __device__ __forceinline__ Cut find_cut(KeepRoom &room, const uint32_t (&key)[kV
         room.bins[blockDim.x + threadIdx.x] = 0;
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kVecs * 4; ++e) {
-            const uint32_t v = key[e] - lo, bin = v >> shift;
-            const unsigned long long in = __ballot(v <= range);
-            if (in != 0) {
-                const unsigned long long same = __ballot(bin == of_lane(bin, __builtin_ctzll(in))) & in;
-                const unsigned long long leader = same & (0ull - same);
-                if (((in & ~same) | leader) >> lane & 1) atomicAdd(&room.bins[bin], (leader >> lane & 1) != 0 ? (uint32_t)__popcll(same) : 1u);
+        for (int v = 0; v < kVecs; ++v) {
+            const uint32_t bin0 = (key[v * 4] - lo) >> shift;
+            const unsigned long long in0 = __ballot(key[v * 4] - lo <= range);
+            const unsigned long long same0 = in0 != 0 ? __ballot(bin0 == of_lane(bin0, __builtin_ctzll(in0))) & in0 : 0ull;
+            if (__popcll(same0) <= 8) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (key[v * 4 + j] - lo <= range) atomicAdd(&room.bins[(key[v * 4 + j] - lo) >> shift], 1u);
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t u = (j == 0 ? key[v * 4] : j == 1 ? key[v * 4 + 1] : j == 2 ? key[v * 4 + 2] : key[v * 4 + 3]) - lo, bin = u >> shift;
+                    const unsigned long long in = __ballot(u <= range);
+                    if (in == 0) continue;
+                    const unsigned long long same = __ballot(bin == of_lane(bin, __builtin_ctzll(in))) & in, leader = same & (0ull - same);
+                    if (((in & ~same) | leader) >> lane & 1) atomicAdd(&room.bins[bin], (leader >> lane & 1) != 0 ? (uint32_t)__popcll(same) : 1u);
+                }
             }
         }
         __syncthreads();
@@ -234,7 +244,8 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int n = slots_of(a, sequence), k = min(n, a.budget);
     const long long base = (long long)frame * a.n_max;
-    const int length = a.lengths != nullptr ? a.lengths[sequence] : n;
+    const long long since = (long long)(a.lengths != nullptr ? a.lengths[sequence] : n) - a.recent;  // places at or beyond it are protected
+    const int newest = since < INT32_MIN ? INT32_MIN : (int)since;
     const int base_slot = wave * (256 * kVecs) + lane * 4;
     auto slot_of = [&](int e) { return base_slot + (e >> 2) * 256 + (e & 3); };
     const bool whole = (wave + 1) * (256 * kVecs) <= n;  // of the wavefront: every slot holds a row
@@ -242,7 +253,7 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     auto take = [&](int v, const Four<float> &s, const Four<int32_t> &p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool protect = p.v[j] < a.first || (long long)p.v[j] >= (long long)length - a.recent;
+            const bool protect = p.v[j] < a.first || p.v[j] >= newest;
             const uint32_t u = live_key(s.v[j], protect);
             const bool there = whole || base_slot + v * 256 + j < n;
             key[v * 4 + j] = there ? u : 0u;
