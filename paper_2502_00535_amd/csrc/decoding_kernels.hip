@@ -29,6 +29,7 @@ __device__ __forceinline__ int frame_count(const int32_t *counts, int s, int n_m
 #include "kernels/verify.h"
 #include "kernels/cache_move.h"
 #include "kernels/cache_keep.h"
+#include "kernels/cache_split.h"
 
 // ----------------------------------------------------------------------------- host side
 
@@ -102,7 +103,7 @@ WeightArgs weight_args(const nms_cache_weights *w)
 int add_launch(const CacheArgs &a, const WeightArgs &w, int type, int frames, hipStream_t stream)
 {
     const int columns = w.columns < a.n_max ? w.columns : a.n_max;
-    const dim3 grid((columns + 255) / 256, frames), block(kAddWaves * 64);
+    const dim3 grid((columns + kAddSlots - 1) / kAddSlots, frames), block(kAddWaves * 64);
     begin_launch();
     if (type == NMS_TYPE_F32) cache_add_kernel<float><<<grid, block, 0, stream>>>(a, w);
     else if (type == NMS_TYPE_F16) cache_add_kernel<_Float16><<<grid, block, 0, stream>>>(a, w);
@@ -114,7 +115,7 @@ template <int kVecs>
 int keep_launch(const CacheArgs &a, const WeightArgs &w, int type, const MoveArgs &m, int frames, hipStream_t stream)
 {
     const dim3 grid(frames), block((a.n_max + 256 * kVecs - 1) / (256 * kVecs) * 64);
-    const size_t lds = (size_t)a.moves_max * sizeof(uint16_t);
+    const size_t lds = (size_t)a.moves_max * (2 * sizeof(uint16_t) + (w.weights != nullptr ? sizeof(float) : 0));
     begin_launch();
     if constexpr (kVecs <= 4) {
         if (w.weights != nullptr) {
@@ -144,27 +145,49 @@ MoveArgs move_args(const int32_t *moves, int n_max, int heads, int budget, const
 
 int move_launch(const MoveArgs &m, int frames, hipStream_t stream)
 {
-    if (m.moves_max == 0 || m.n_tensors == 0) return NMS_OK;
+    if (m.moves_max == 0 || (m.n_tensors == 0 && m.sums == nullptr)) return NMS_OK;
     begin_launch();
     cache_move_kernel<<<dim3((m.moves_max + kMoveRows - 1) / kMoveRows, frames), dim3(256), 0, stream>>>(m);
     return launch_status();
 }
 
+// The keep vector and the moves of frames that several workgroups share.
+int split_launch(const CacheArgs &a, void *scratch, int frames, hipStream_t stream)
+{
+    const NmsSplitLayout at = nms_split_layout(a.n_max, frames);
+    char *room = static_cast<char *>(scratch);
+    SplitArgs x = {reinterpret_cast<uint32_t *>(room + at.keys), reinterpret_cast<uint16_t *>(room + at.bins),
+                   reinterpret_cast<unsigned long long *>(room + at.cuts), reinterpret_cast<uint32_t *>(room + at.stays), at.parts, at.part};
+    const dim3 grid(at.parts, frames), block(kSplitThreads);
+    begin_launch();
+    cache_split_keys_kernel<<<grid, block, 0, stream>>>(a, x);
+    int st = launch_status();
+    if (st != NMS_OK) return st;
+    begin_launch();
+    cache_split_cut_kernel<<<dim3(frames), dim3(kCutThreads), 0, stream>>>(a, x);
+    st = launch_status();
+    if (st != NMS_OK) return st;
+    begin_launch();
+    cache_split_keep_kernel<<<grid, block, 0, stream>>>(a, x);
+    return launch_status();
+}
+
 // The keep vector and the moves; rows of `m` move in the same launch where there are few, by one of their own otherwise.
-int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const MoveArgs &m, int frames, hipStream_t stream)
+int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const MoveArgs &m, void *scratch, int frames, hipStream_t stream)
 {
     WeightArgs w = weight_args(weights);
     const int type = weights != nullptr ? weights->type : 0;
-    if (w.weights != nullptr && !nms_cache_add_with_keep(a.n_max, w.group * (long long)w.tokens)) {
+    if (w.weights != nullptr && !nms_cache_add_with_keep(a.n_max, frames, w.group * (long long)w.tokens)) {
         const int st = add_launch(a, w, type, frames, stream);
         if (st != NMS_OK) return st;
         w = {};
     }
-    if (a.n_max > kKeepMaxWaves * 256 * 16) {
-        begin_launch();
-        cache_keep_long_kernel<<<dim3(frames), dim3(kKeepThreads), 0, stream>>>(a);
-        const int st = launch_status();
-        return st != NMS_OK ? st : move_launch(m, frames, stream);
+    if (nms_cache_split(a.n_max, frames)) {
+        const int st = split_launch(a, scratch, frames, stream);
+        if (st != NMS_OK) return st;
+        MoveArgs with_sums = m;
+        if (a.move_sums) with_sums.sums = a.sums, with_sums.positions = a.positions;
+        return move_launch(with_sums, frames, stream);
     }
     const bool few = a.moves_max <= kFew;
     CacheArgs b = a;
@@ -175,8 +198,7 @@ int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const Mo
     case 1: st = keep_launch<1>(b, w, type, now, frames, stream); break;
     case 2: st = keep_launch<2>(b, w, type, now, frames, stream); break;
     case 4: st = keep_launch<4>(b, w, type, now, frames, stream); break;
-    case 8: st = keep_launch<8>(b, w, type, now, frames, stream); break;
-    default: st = keep_launch<16>(b, w, type, now, frames, stream); break;
+    default: st = keep_launch<8>(b, w, type, now, frames, stream); break;
     }
     return st != NMS_OK || few ? st : move_launch(m, frames, stream);
 }
@@ -239,7 +261,7 @@ int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t 
     if (st != NMS_OK) return st;
     const CacheArgs a = {sums, const_cast<int32_t *>(positions), counts, lengths, keep_out, kept_out, moves_out, n_max, heads, budget, first, recent,
                          nms_moves_max(n_max, budget), false};
-    return keep_and_move(a, weights, MoveArgs{}, heads * sequences, static_cast<hipStream_t>(stream));
+    return keep_and_move(a, weights, MoveArgs{}, workspace, heads * sequences, static_cast<hipStream_t>(stream));
 }
 
 int nms_cache_move_batched(const int32_t *moves, int n_max, int heads, int sequences, int budget, const nms_cache_tensor *tensors,
@@ -271,10 +293,12 @@ int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *coun
     st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
     if (st != NMS_OK) return st;
     const int frames = heads * sequences;
+    // the list of moves first, then what finds it
     int32_t *moves = static_cast<int32_t *>(workspace);
+    void *scratch = static_cast<char *>(workspace) + nms_cache_list_bytes(n_max, frames, budget);
     const CacheArgs a = {sums, positions, counts, lengths, keep_out, kept_out, moves, n_max, heads, budget, first, recent,
                          nms_moves_max(n_max, budget), true};
-    return keep_and_move(a, weights, move_args(moves, n_max, heads, budget, tensors, n_tensors, pages), frames, static_cast<hipStream_t>(stream));
+    return keep_and_move(a, weights, move_args(moves, n_max, heads, budget, tensors, n_tensors, pages), scratch, frames, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -43,14 +43,31 @@ __device__ __forceinline__ double as_weight(T v)
 template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
 
+// Elements at or beyond `end` come out as 0.  The last vector is loaded from four elements before the end and shifted, so that a wavefront at the row's
+// end has no branch to wait in (element by element such wavefronts took 26 us where the others took 10, at 8 x 4001 slots with 32 query rows).
 template <typename T>
 __device__ __forceinline__ Four<T> load_four(const T *row, int i, int end)
 {
-    if (i + 4 <= end) return *reinterpret_cast<const Four<T> *>(row + i);
     Four<T> r = {};
+    if (end < 4) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (i + j < end) r.v[j] = row[i + j];
+        for (int j = 0; j < 3; ++j)
+            if (i + j < end) r.v[j] = row[i + j];
+        return r;
+    }
+    const int at = min(i, end - 4), d = i - at;
+    r = *reinterpret_cast<const Four<T> *>(row + at);
+    if constexpr (sizeof(T) == 2) {
+        unsigned long long x;
+        __builtin_memcpy(&x, &r, sizeof x);
+        x = d < 4 ? x >> (16 * d) : 0ull;
+        __builtin_memcpy(&r, &x, sizeof x);
+    } else {
+        r.v[0] = d == 0 ? r.v[0] : d == 1 ? r.v[1] : d == 2 ? r.v[2] : d == 3 ? r.v[3] : T{};
+        r.v[1] = d == 0 ? r.v[1] : d == 1 ? r.v[2] : d == 2 ? r.v[3] : T{};
+        r.v[2] = d == 0 ? r.v[2] : d == 1 ? r.v[3] : T{};
+        r.v[3] = d == 0 ? r.v[3] : T{};
+    }
     return r;
 }
 template <typename T>
@@ -67,15 +84,17 @@ __device__ __forceinline__ void store_four(T *row, int i, int end, const Four<T>
 
 // sums[i] += the weights of slot i, by a launch of its own where there are many query rows: a wavefront has 256 neighbouring slots, the four
 // wavefronts of a workgroup share out the rows, and their sums in 64 bits meet in LDS in the same order always.  Bound by the weights'
-// bytes: eight rows are in flight to a lane.
-constexpr int kAddWaves = 4;
+// bytes: eight rows are in flight to a lane (8 heads x 100,003 slots x 128 rows of bf16 58 us, 3.5 TB/s; eight slots to a lane, for 16-byte loads,
+// and four rows in flight took 58 to 64 us, sixteen rows in flight 58).
+constexpr int kAddWaves = 4, kAddSlots = 256;
 template <typename T>
 __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, WeightArgs w)
 {
     __shared__ double room[kAddWaves - 1][4][64];
     const int frame = blockIdx.y, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = min(slots_of(a, sequence), w.columns), i = blockIdx.x * 256 + lane * 4;
-    if ((int)blockIdx.x * 256 >= n) return;
+    const int n = min(slots_of(a, sequence), w.columns), i = blockIdx.x * kAddSlots + lane * 4;
+    if ((int)blockIdx.x * kAddSlots >= n) return;
+    const bool whole = (int)(blockIdx.x + 1) * kAddSlots <= n;
     const int tokens = valid_of(w, sequence), rows = w.group * tokens;
     const T *first = static_cast<const T *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
@@ -84,22 +103,24 @@ __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, 
         Four<T> x[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const int r = min(r0 + u * kAddWaves, rows - 1), g = r / tokens;
-            x[u] = load_four(first + ((long long)g * w.tokens + (r - g * tokens)) * w.row_stride, i, n);
+            const int r = r0 + u * kAddWaves, g = r / tokens;
+            x[u] = {};
+            if (r < rows) {
+                const T *at = first + ((long long)g * w.tokens + (r - g * tokens)) * w.row_stride;
+                x[u] = whole ? *reinterpret_cast<const Four<T> *>(at + i) : load_four(at, i, n);
+            }
         }
 #pragma unroll
         for (int u = 0; u < kRows; ++u)
-            if (r0 + u * kAddWaves < rows) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j] += as_weight(x[u].v[j]);
-            }
+            for (int j = 0; j < 4; ++j) sum[j] += as_weight(x[u].v[j]);
     }
     if (wave > 0) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) room[wave - 1][j][lane] = sum[j];
     }
     __syncthreads();
-    if (wave > 0 || i >= n) return;
+    if (wave > 0) return;
     float *sums = a.sums + (long long)frame * a.n_max;
     Four<float> s = load_four(sums, i, n);
 #pragma unroll
@@ -145,7 +166,6 @@ struct KeepRoom {
     uint32_t wave_a[kKeepMaxWaves], wave_b[kKeepMaxWaves], wave_c[kKeepMaxWaves];
     uint32_t found[3];             // bin, how many lie beyond it, how many in it
     uint32_t few, few_keys[kFew];
-    uint16_t from[kFew];
 };
 
 // Where the best `need` of the `left` keys between lo and hi end (0 < need <= left): at the least that stays, and how many keys equal to it are
@@ -240,7 +260,9 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     constexpr int kEach = kVecs * 4;
     constexpr bool kWeights = !std::is_same<W, void>::value;
     __shared__ KeepRoom room;
-    extern __shared__ uint16_t targets[];  // free slots in their order, moves_max of them
+    extern __shared__ float moved_sums[];  // (with weights) moves_max of them, of
+    uint16_t *targets = reinterpret_cast<uint16_t *>(moved_sums + (kWeights ? a.moves_max : 0));  // rows that move into these slots, in order,
+    uint16_t *sources = targets + a.moves_max;                                                     // from these
     const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int n = slots_of(a, sequence), k = min(n, a.budget);
     const long long base = (long long)frame * a.n_max;
@@ -271,9 +293,13 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         const int i = base_slot + v * 256;
         return whole ? *reinterpret_cast<const Four<float> *>(a.sums + base + i) : load_four(a.sums + base, i, n);
     };
+    float sum[kWeights ? kEach : 1];  // with weights: the new sums, in memory only once their places are known
     if constexpr (kWeights) {
-        const int columns = min(n, w.columns), tokens = valid_of(w, sequence);
-        const W *row = static_cast<const W *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
+        constexpr int kRows = kVecs < 4 ? 4 : 2;  // query rows in flight
+        const int columns = min(n, w.columns), tokens = valid_of(w, sequence), rows = w.group * tokens;
+        const bool all = (wave + 1) * (256 * kVecs) <= columns;
+        const long long gap = (long long)(w.tokens - tokens) * w.row_stride;  // between the valid rows of two query heads
+        const W *at = static_cast<const W *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
         Four<int32_t> p[kVecs];
         Four<float> s[kVecs];
         double total[kEach];
@@ -283,24 +309,32 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         for (int v = 0; v < kVecs; ++v) p[v] = places(v);
 #pragma unroll
         for (int e = 0; e < kEach; ++e) total[e] = (double)s[e >> 2].v[e & 3];
-        const bool all = (wave + 1) * (256 * kVecs) <= columns;
-        for (int g = 0; g < w.group; ++g)
-            for (int t = 0; t < tokens; ++t) {
-                const W *at = row + ((long long)g * w.tokens + t) * w.row_stride;
-                Four<W> x[kVecs];
+        for (int r = 0, t = 0; r < rows; r += kRows) {
+            Four<W> x[kRows][kVecs];
 #pragma unroll
-                for (int v = 0; v < kVecs; ++v) {
-                    const int i = base_slot + v * 256;
-                    x[v] = all ? *reinterpret_cast<const Four<W> *>(at + i) : load_four(at, i, columns);
+            for (int u = 0; u < kRows; ++u) {
+                if (r + u < rows) {
+#pragma unroll
+                    for (int v = 0; v < kVecs; ++v) {
+                        const int i = base_slot + v * 256;
+                        x[u][v] = all ? *reinterpret_cast<const Four<W> *>(at + i) : load_four(at, i, columns);
+                    }
+                    at += w.row_stride;
+                    if (++t == tokens) t = 0, at += gap;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < kVecs; ++v) x[u][v] = {};
                 }
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) total[e] += as_weight(x[e >> 2].v[e & 3]);
             }
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) total[e] += as_weight(x[u][e >> 2].v[e & 3]);
+        }
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[v].v[j] = (float)total[v * 4 + j];
-            store_four(a.sums + base, base_slot + v * 256, n, s[v]);
+            for (int j = 0; j < 4; ++j) sum[v * 4 + j] = s[v].v[j] = (float)total[v * 4 + j];
             take(v, s[v], p[v]);
         }
     } else {
@@ -339,7 +373,7 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         uint32_t lo = ~smallest, hi = largest, need = (uint32_t)k - guarded, left = (uint32_t)n - guarded;
         if ((uint32_t)k <= guarded) lo = hi = NMS_CACHE_KEY_PROTECTED, need = (uint32_t)k, left = guarded;  // protected rows alone
         Cut cut;
-        for (int stage = 0;; ++stage) {
+        for (;;) {
             cut = find_cut<kVecs>(room, key, lo, hi, need, left, wave, lane);
             const bool ties = cut.wanted < cut.there;
 #pragma unroll
@@ -351,174 +385,94 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
             lo = ~(uint32_t)(waves * 256 * kVecs - 1), hi = ~0u, need = cut.wanted, left = cut.there;
         }
     }
-    if (a.keep != nullptr) {
+    // moves: slots below k whose row goes are free, rows that stay beyond take them in order
+    uint32_t total = 0;
+    if (a.moves_max > 0 && (a.moves != nullptr || a.move_sums)) {
+        Bits is_free = 0, moves = 0;
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
+        for (int e = 0; e < kEach; ++e) {
+            const bool s = stay >> e & 1, low = slot_of(e) < k;
+            is_free |= (Bits)(low && !s) << e;
+            moves |= (Bits)(!low && s) << e;
+        }
+        const uint32_t counts = wave_running_count((uint32_t)__popcll(is_free) << 16 | (uint32_t)__popcll(moves));  // at most 2048 of each in a wavefront
+        if (lane == 63) room.wave_b[wave] = counts;
+        __syncthreads();
+        uint32_t to = 0, from = 0;
+        for (int i = 0; i < waves; ++i) {
+            const uint32_t c = room.wave_b[i];
+            to += i < wave ? c >> 16 : 0u;
+            from += i < wave ? c & 0xffffu : 0u;
+            total += c & 0xffffu;
+        }
+        // in order of slots: visit(element, its rank) for each of the flagged
+        auto ranked = [&](Bits flags, uint32_t rank0, auto &&visit) {
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) {
+                const uint32_t own = (uint32_t)(flags >> (v * 4)) & 15u;
+                if (__ballot(own != 0) == 0) continue;
+                const uint32_t upto = wave_running_count(__popc(own));
+                uint32_t rank = rank0 + upto - __popc(own);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (own >> j & 1) visit(v * 4 + j, rank++);
+                rank0 += of_lane(upto, 63);
+            }
+        };
+        ranked(is_free, to, [&](int e, uint32_t r) { targets[r] = (uint16_t)slot_of(e); });
+        ranked(moves, from, [&](int e, uint32_t r) {
+            sources[r] = (uint16_t)slot_of(e);
+            if constexpr (kWeights) moved_sums[r] = sum[e];
+        });
+        __syncthreads();
+        // no two of the stores below have an address in common, so that none of them waits for another
+        for (uint32_t r = threadIdx.x; r < total; r += blockDim.x) {
+            const int t = targets[r], i = sources[r];
+            if (a.moves != nullptr) reinterpret_cast<int2 *>(a.moves)[(long long)frame * (a.moves_max + 1) + 1 + r] = make_int2(t, i);
+            if (a.move_sums) {
+                float s;
+                if constexpr (kWeights) s = moved_sums[r];
+                else s = a.sums[base + i];
+                if (a.positions != nullptr) a.positions[base + t] = a.positions[base + i];
+                a.sums[base + t] = s;
+                a.sums[base + i] = 0.0f;
+            }
+        }
+    }
+    if (a.moves != nullptr && threadIdx.x == 0) reinterpret_cast<int2 *>(a.moves)[(long long)frame * (a.moves_max + 1)] = make_int2((int)total, 0);
+    if (a.kept != nullptr && threadIdx.x == 0 && frame % a.heads == 0) a.kept[sequence] = k;
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+        const int i = base_slot + v * 256;
+        const uint32_t flags = (uint32_t)(stay >> (v * 4)) & 15u;
+        if (a.keep != nullptr) {
             Four<uint8_t> f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f.v[j] = stay >> (v * 4 + j) & 1;
-            store_four(a.keep + base, base_slot + v * 256, a.n_max, f);
+            for (int j = 0; j < 4; ++j) f.v[j] = flags >> j & 1;
+            store_four(a.keep + base, i, a.n_max, f);
         }
-    }
-    if (a.kept != nullptr && threadIdx.x == 0 && frame % a.heads == 0) a.kept[sequence] = k;
-    if (a.moves == nullptr && !a.move_sums) return;
-    // moves: slots below k whose row goes are free, rows that stay beyond take them in order
-    Bits is_free = 0, moves = 0;
+        // sums: new ones with weights, 0 for rows that go from slots at or beyond k; slots of moves are written above
+        if (kWeights && !a.move_sums) {
+            Four<float> s;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        const bool s = stay >> e & 1, low = slot_of(e) < k;
-        is_free |= (Bits)(low && !s) << e;
-        moves |= (Bits)(!low && s) << e;
-    }
-    const uint32_t counts = wave_running_count((uint32_t)__popcll(is_free) << 16 | (uint32_t)__popcll(moves));  // at most 4096 of each in a wavefront
-    if (lane == 63) room.wave_b[wave] = counts;
-    __syncthreads();
-    uint32_t to = 0, from = 0, total = 0;
-    for (int i = 0; i < waves; ++i) {
-        const uint32_t c = room.wave_b[i];
-        to += i < wave ? c >> 16 : 0u;
-        from += i < wave ? c & 0xffffu : 0u;
-        total += c & 0xffffu;
-    }
-    // in order of slots: visit(element, its rank) for each of the flagged
-    auto ranked = [&](Bits flags, uint32_t rank0, auto &&visit) {
+            for (int j = 0; j < 4; ++j) s.v[j] = kWeights ? sum[kWeights ? v * 4 + j : 0] : 0.0f;
+            store_four(a.sums + base, i, n, s);
+        } else if (a.move_sums && (kWeights || i + 4 > k)) {
+            if (kWeights && flags == 15u && i + 4 <= k) {
+                Four<float> s;
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-            const uint32_t own = (uint32_t)(flags >> (v * 4)) & 15u;
-            if (__ballot(own != 0) == 0) continue;
-            const uint32_t upto = wave_running_count(__popc(own));
-            uint32_t rank = rank0 + upto - __popc(own);
+                for (int j = 0; j < 4; ++j) s.v[j] = kWeights ? sum[kWeights ? v * 4 + j : 0] : 0.0f;
+                store_four(a.sums + base, i, n, s);
+            } else if (flags == 0u && i >= k) {
+                store_four(a.sums + base, i, n, Four<float>{});
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (own >> j & 1) visit(v * 4 + j, rank++);
-            rank0 += of_lane(upto, 63);
-        }
-    };
-    ranked(is_free, to, [&](int e, uint32_t r) { targets[r] = (uint16_t)slot_of(e); });
-    __syncthreads();
-    int2 *list = a.moves != nullptr ? reinterpret_cast<int2 *>(a.moves) + (long long)frame * (a.moves_max + 1) : nullptr;
-    if (list != nullptr && threadIdx.x == 0) list[0] = make_int2((int)total, 0);
-    ranked(moves, from, [&](int e, uint32_t r) {
-        const int t = targets[r], i = slot_of(e);
-        if (list != nullptr) list[1 + r] = make_int2(t, i);
-        if (r < (uint32_t)kFew) room.from[r] = (uint16_t)i;
-        if (a.move_sums) {
-            a.sums[base + t] = a.sums[base + i];
-            if (a.positions != nullptr) a.positions[base + t] = a.positions[base + i];
-        }
-    });
-    if (!a.move_sums) return;
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) {  // behind the rows that stay: no sums
-        const int i = base_slot + v * 256;
-        if (i >= k) store_four(a.sums + base, i, n, Four<float>{});
-        else if (i + 4 > k) {
-#pragma unroll
-            for (int j = 1; j < 4; ++j)
-                if (i + j >= k && i + j < n) a.sums[base + i + j] = 0.0f;
+                for (int j = 0; j < 4; ++j) {
+                    const bool s = flags >> j & 1;
+                    if (i + j < n && (i + j >= k ? !s : kWeights && s)) a.sums[base + i + j] = i + j >= k ? 0.0f : sum[kWeights ? v * 4 + j : 0];
+                }
+            }
         }
     }
-    if (m.n_tensors > 0) move_rows(m, frame, (int)total, (int)blockDim.x, [&](int r) { return make_int2(targets[r], room.from[r]); });  // few rows: in this launch
-}
-
-constexpr int kKeepThreads = 1024;
-constexpr int kKeepWaves = kKeepThreads / 64;
-
-// Sum of one number per wavefront over the workgroup, and of the wavefronts before one's own.
-__device__ __forceinline__ int2 across_waves(int v, int *room, int wave, int lane)
-{
-    __syncthreads();
-    if (lane == 0) room[wave] = v;
-    __syncthreads();
-    int2 r = make_int2(0, 0);
-    for (int i = 0; i < kKeepWaves; ++i) {
-        r.x += room[i];
-        r.y += i < wave ? room[i] : 0;
-    }
-    return r;
-}
-
-// Frames of more slots than a workgroup's registers hold.  The key that parts the rows that stay from those that go is found bit by bit from the top: the largest T with at
-// least k keys >= T.  Keys above T stay, and of those equal to it the lowest slots.  Each wavefront has a stretch of neighbouring slots, so that
-// ranks among slots are counts of lanes before one's own.
-__global__ void __launch_bounds__(kKeepThreads) cache_keep_long_kernel(CacheArgs a)
-{
-    __shared__ int room[kKeepWaves];
-    const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = slots_of(a, sequence), k = min(n, a.budget);
-    const long long base = (long long)frame * a.n_max;
-    const int length = a.lengths != nullptr ? a.lengths[sequence] : n;
-    const int stretch = (n + kKeepThreads - 1) / kKeepThreads * 64;
-    const int begin = min(wave * stretch, n), end = min(begin + stretch, n);
-    auto key = [&](int i) {
-        const int position = a.positions != nullptr ? a.positions[base + i] : i;
-        const bool protect = position < a.first || (long long)position >= (long long)length - a.recent;
-        return protect ? NMS_CACHE_KEY_PROTECTED : nms_cache_key_bits(__float_as_uint(a.sums[base + i]));
-    };
-    uint32_t threshold = 0;
-    int above = 0;  // keys beyond the threshold
-    if (k < n && k > 0) {
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t test = threshold | (1u << bit);
-            int c = 0;
-            for (int i = begin + lane; i < end; i += 64) c += key(i) >= test;
-            for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d);
-            if (across_waves(c, room, wave, lane).x >= k) threshold = test;
-        }
-        int c = 0;
-        for (int i = begin + lane; i < end; i += 64) c += key(i) > threshold;
-        for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d);
-        above = across_waves(c, room, wave, lane).x;
-    }
-    const int ties = k == n ? n : k - above;  // of the keys at the threshold, how many stay (k == n: all of them, whatever their keys)
-    const bool none = k == 0;
-    auto pass = [&](auto &&visit, int ties_before) {
-        int seen = ties_before;
-        for (int i0 = begin; i0 < end; i0 += 64) {
-            const int i = i0 + lane;
-            const uint32_t u = i < end ? key(i) : 0u;
-            const bool equal = i < end && (k == n || u == threshold);
-            const unsigned long long mask = __ballot(equal);
-            const int rank = seen + __popcll(mask & ((1ull << lane) - 1));
-            seen += __popcll(mask);
-            visit(i, i < end && !none && (equal ? rank < ties : k < n && u > threshold));
-        }
-        return seen;
-    };
-    int c = 0;
-    for (int i = begin + lane; i < end; i += 64) c += k == n || key(i) == threshold;
-    for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d);
-    const int ties_before = across_waves(c, room, wave, lane).y;
-    int free_slots = 0, moved = 0;
-    pass([&](int i, bool stays) {
-        free_slots += __popcll(__ballot(i < end && i < k && !stays));
-        moved += __popcll(__ballot(i >= k && stays));
-        if (a.keep != nullptr && i < end) a.keep[base + i] = stays;
-    }, ties_before);
-    if (a.keep != nullptr)
-        for (int i = n + threadIdx.x; i < a.n_max; i += kKeepThreads) a.keep[base + i] = 0;
-    if (a.kept != nullptr && threadIdx.x == 0 && frame % a.heads == 0) a.kept[sequence] = k;
-    if (a.moves == nullptr) return;
-    int32_t *list = a.moves + (long long)frame * (a.moves_max + 1) * 2;
-    const int2 f = across_waves(free_slots, room, wave, lane), m = across_waves(moved, room, wave, lane);
-    if (threadIdx.x == 0) list[0] = m.x, list[1] = 0;
-    int to = f.y, from = m.y;
-    pass([&](int i, bool stays) {
-        const bool is_free = i < end && i < k && !stays, moves = i >= k && stays;
-        const unsigned long long mf = __ballot(is_free), mm = __ballot(moves), before = (1ull << lane) - 1;
-        if (is_free) list[2 + 2 * (to + __popcll(mf & before))] = i;
-        if (moves) list[3 + 2 * (from + __popcll(mm & before))] = i;
-        to += __popcll(mf);
-        from += __popcll(mm);
-    }, ties_before);
-    if (!a.move_sums) return;
-    __syncthreads();
-    for (int r = threadIdx.x; r < m.x; r += kKeepThreads) {
-        const int t = list[2 + 2 * r], s = list[3 + 2 * r];
-        a.sums[base + t] = a.sums[base + s];
-        if (a.positions != nullptr) a.positions[base + t] = a.positions[base + s];
-    }
-    __syncthreads();
-    for (int i = k + threadIdx.x; i < n; i += kKeepThreads) a.sums[base + i] = 0.0f;
+    if (m.n_tensors > 0) move_rows(m, frame, (int)total, (int)blockDim.x, [&](int r) { return make_int2(targets[r], sources[r]); });  // few rows: in this launch
 }

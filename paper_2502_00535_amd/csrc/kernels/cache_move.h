@@ -10,6 +10,8 @@ struct MoveTensor {
 };
 struct MoveArgs {
     const int32_t *moves;
+    float *sums;          // of long frames: they and the positions move with the rows, and the places that they leave are set to 0
+    int32_t *positions;
     int n_max, heads, budget, moves_max, n_tensors;
     nms_cache_pages pages;
     MoveTensor tensors[NMS_CACHE_MAX_TENSORS];
@@ -52,5 +54,13 @@ __global__ void __launch_bounds__(256) cache_move_kernel(MoveArgs a)
     const int frame = blockIdx.y;
     const int2 *list = reinterpret_cast<const int2 *>(a.moves) + (long long)frame * (a.moves_max + 1);
     const int begin = blockIdx.x * kMoveRows, rows = min(min(list[0].x, a.moves_max) - begin, kMoveRows);
-    if (rows > 0) move_rows(a, frame, rows, 256, [&](int r) { return list[1 + begin + r]; });
+    if (rows <= 0) return;
+    if (a.sums != nullptr && threadIdx.x < (unsigned)rows) {
+        const int2 pair = list[1 + begin + threadIdx.x];
+        const long long base = (long long)frame * a.n_max;
+        a.sums[base + pair.x] = a.sums[base + pair.y];
+        a.sums[base + pair.y] = 0.0f;
+        if (a.positions != nullptr) a.positions[base + pair.x] = a.positions[base + pair.y];
+    }
+    move_rows(a, frame, rows, 256, [&](int r) { return list[1 + begin + r]; });
 }

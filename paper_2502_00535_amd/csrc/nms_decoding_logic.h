@@ -1,3 +1,9 @@
+#ifndef NMS_SPLIT
+#define NMS_SPLIT (n_max > 32768 || (n_max > 16384 && frames <= 32))
+#endif
+#ifndef NMS_FUSE
+#define NMS_FUSE (rows <= 32)
+#endif
 // Host-checkable logic of the decoding step's choices (verification of drafted tokens, eviction from a cache): keys,
 // sizes, workspace layout and addresses.  Compiled by hipcc for the library and by a plain host compiler for the tests.
 #ifndef NMS_DECODING_LOGIC_H
@@ -35,14 +41,10 @@ NMS_HD int nms_moves_max(int n_max, int budget)
     return budget < behind ? budget : behind;
 }
 static inline size_t nms_decoding_align256(size_t v) { return (v + 255) & ~(size_t)255; }
-// Scratch of the whole path: the list of moves.
-static inline size_t nms_cache_scratch(int n_max, int frames, int budget)
-{
-    return nms_decoding_align256((size_t)frames * ((size_t)nms_moves_max(n_max, budget) + 1) * 2 * sizeof(int32_t));
-}
-
 // ---- eviction: the route ------------------------------------------------------------------------
-// Vectors of four slots to a lane: a frame is one workgroup of at most sixteen wavefronts.
+// Frames longer than a workgroup's registers hold are shared by several workgroups, in three launches.
+static inline bool nms_cache_split(int n_max, int frames) { return NMS_SPLIT; }
+// Else: vectors of four slots to a lane, a frame is one workgroup of at most sixteen wavefronts.
 static inline int nms_cache_vecs(int n_max)
 {
     int vecs = n_max <= 1024 ? 1 : 2;
@@ -50,7 +52,37 @@ static inline int nms_cache_vecs(int n_max)
     return vecs;
 }
 // The weights are added by the launch that finds the rows that stay where there are few query rows, by one of its own otherwise.
-static inline bool nms_cache_add_with_keep(int n_max, long long rows) { return rows <= 32 && nms_cache_vecs(n_max) <= 4; }
+static inline bool nms_cache_add_with_keep(int n_max, int frames, long long rows)
+{
+    return !nms_cache_split(n_max, frames) && NMS_FUSE && nms_cache_vecs(n_max) <= 4;
+}
+
+// Scratch: the list of moves (of the whole path), and what the three launches hand on.
+static inline size_t nms_cache_list_bytes(int n_max, int frames, int budget)
+{
+    return nms_decoding_align256((size_t)frames * ((size_t)nms_moves_max(n_max, budget) + 1) * 2 * sizeof(int32_t));
+}
+struct NmsSplitLayout {
+    int part, parts;                       // slots to a part, most parts to a frame
+    size_t keys, bins, cuts, stays, bytes; // offsets, and all of it
+};
+static inline NmsSplitLayout nms_split_layout(int n_max, int frames)
+{
+    NmsSplitLayout l;
+    l.part = 4096;  // the largest part that still makes two workgroups to a compute unit
+    while (l.part > 1024 && (long long)frames * (n_max / l.part) < 512) l.part /= 2;
+    l.parts = (n_max + l.part - 1) / l.part + 1;
+    l.keys = 0;
+    l.bins = l.keys + nms_decoding_align256((size_t)frames * n_max * sizeof(uint32_t));
+    l.cuts = l.bins + nms_decoding_align256((size_t)frames * l.parts * 2048 * sizeof(uint16_t));
+    l.stays = l.cuts + nms_decoding_align256((size_t)frames * sizeof(uint64_t));
+    l.bytes = l.stays + nms_decoding_align256((size_t)frames * l.parts * sizeof(uint32_t));
+    return l;
+}
+static inline size_t nms_cache_scratch(int n_max, int frames, int budget)
+{
+    return nms_cache_list_bytes(n_max, frames, budget) + (nms_cache_split(n_max, frames) ? nms_split_layout(n_max, frames).bytes : 0);
+}
 
 // ---- verification: the cut of a row, and the route -------------------------------------------
 #define NMS_VERIFY_SEGMENT 2048
