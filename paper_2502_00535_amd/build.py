@@ -19,17 +19,24 @@ MARSHAL = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"
 
 # -ffp-contract=off: the pair test must round every operation on its own (the one
 #   fused multiply-add it uses is written explicitly).
-# -fno-honor-nans (device only): inputs are NaN-free by contract; without it every
-#   min/max operand fetched from memory is first re-quieted with an extra VALU
-#   instruction.  Host code keeps full NaN semantics for argument checking.
+# -fno-honor-nans (device only, and only where inputs are NaN-free by contract): without
+#   it every min/max operand fetched from memory is first re-quieted with an extra VALU
+#   instruction.  Host code keeps full NaN semantics for argument checking.  Attention
+#   weights and probabilities may hold NaN, so the decoding kernels do without.
 # -packed-fp32-ops off: no packed float32 VALU instructions are generated.
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-ffp-contract=off",
-    "-Xarch_device", "-fno-honor-nans",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
 ]
+
+
+NAN_FREE_FLAGS = ["-Xarch_device", "-fno-honor-nans"]
+
+
+def _flags(source: str) -> list[str]:
+    return HIPCC_FLAGS + (NAN_FREE_FLAGS if os.path.basename(source) == "nms_kernels.hip" else [])
 
 
 def is_stale() -> bool:
@@ -80,7 +87,7 @@ def build_library(verbose: bool = False) -> str:
     tmp = LIBRARY + f".tmp{os.getpid()}"
     objects = [tmp + f".{i}.o" for i in range(len(SOURCES))]
     try:
-        messages = _hipcc(*([hipcc, *HIPCC_FLAGS, "-c", source, "-o", obj] for source, obj in zip(SOURCES, objects)))
+        messages = _hipcc(*([hipcc, *_flags(source), "-c", source, "-o", obj] for source, obj in zip(SOURCES, objects)))
         messages += _hipcc([hipcc, *HIPCC_FLAGS, *objects, "-o", tmp])
     finally:
         for obj in objects:

@@ -32,12 +32,14 @@ __device__ __forceinline__ int valid_of(const WeightArgs &w, int sequence)
     return v < 0 ? 0 : min(v, w.tokens);
 }
 
+// Weights that are not finite add nothing.  Looking at each costs more than adding it (8 cycles of 21 to a wavefront), so they are added as they
+// are: a sum in 64 bits of finite floats is finite, and where one comes out that is not the rows are gone over again, with a look at each weight.
 template <typename T>
-__device__ __forceinline__ double as_weight(T v)
+__device__ __forceinline__ T finite_or_none(T v)
 {
-    const float f = to_float(v);
-    return (double)(__builtin_amdgcn_classf(f, 0x1f8) ? f : 0.0f);  // a finite number of either sign
+    return __builtin_amdgcn_classf(to_float(v), 0x1f8) ? v : T{};
 }
+__device__ __forceinline__ bool is_finite(double v) { return (__double2hiint(v) & 0x7ff00000) != 0x7ff00000; }
 
 // Four neighbouring slots of a lane; rows may begin at any element.
 template <typename T>
@@ -97,23 +99,34 @@ __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, 
     const bool whole = (int)(blockIdx.x + 1) * kAddSlots <= n;
     const int tokens = valid_of(w, sequence), rows = w.group * tokens;
     const T *first = static_cast<const T *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
-    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    double sum[4];
     constexpr int kRows = 8;
-    for (int r0 = wave; r0 < rows; r0 += kAddWaves * kRows) {
-        Four<T> x[kRows];
+    for (bool look : {false, true}) {
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            const int r = r0 + u * kAddWaves, g = r / tokens;
-            x[u] = {};
-            if (r < rows) {
-                const T *at = first + ((long long)g * w.tokens + (r - g * tokens)) * w.row_stride;
-                x[u] = whole ? *reinterpret_cast<const Four<T> *>(at + i) : load_four(at, i, n);
+        for (int j = 0; j < 4; ++j) sum[j] = 0.0;
+        for (int r0 = wave; r0 < rows; r0 += kAddWaves * kRows) {
+            Four<T> x[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                const int r = r0 + u * kAddWaves, g = r / tokens;
+                x[u] = {};
+                if (r < rows) {
+                    const T *at = first + ((long long)g * w.tokens + (r - g * tokens)) * w.row_stride;
+                    x[u] = whole ? *reinterpret_cast<const Four<T> *>(at + i) : load_four(at, i, n);
+                }
             }
+            if (look) {
+#pragma unroll
+                for (int u = 0; u < kRows; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[u].v[j] = finite_or_none(x[u].v[j]);
+            }
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += (double)to_float(x[u].v[j]);
         }
-#pragma unroll
-        for (int u = 0; u < kRows; ++u)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += as_weight(x[u].v[j]);
+        if (__ballot(!(is_finite(sum[0]) && is_finite(sum[1]) && is_finite(sum[2]) && is_finite(sum[3]))) == 0) break;
     }
     if (wave > 0) {
 #pragma unroll
@@ -299,7 +312,7 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         const int columns = min(n, w.columns), tokens = valid_of(w, sequence), rows = w.group * tokens;
         const bool all = (wave + 1) * (256 * kVecs) <= columns;
         const long long gap = (long long)(w.tokens - tokens) * w.row_stride;  // between the valid rows of two query heads
-        const W *at = static_cast<const W *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
+        const W *first = static_cast<const W *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
         Four<int32_t> p[kVecs];
         Four<float> s[kVecs];
         double total[kEach];
@@ -307,34 +320,47 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         for (int v = 0; v < kVecs; ++v) s[v] = sums_of(v);
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) p[v] = places(v);
+        for (bool look : {false, true}) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) total[e] = (double)s[e >> 2].v[e & 3];
-        for (int r = 0, t = 0; r < rows; r += kRows) {
-            Four<W> x[kRows][kVecs];
+            for (int e = 0; e < kEach; ++e) total[e] = 0.0;
+            const W *at = first;
+            for (int r = 0, t = 0; r < rows; r += kRows) {
+                Four<W> x[kRows][kVecs];
 #pragma unroll
-            for (int u = 0; u < kRows; ++u) {
-                if (r + u < rows) {
+                for (int u = 0; u < kRows; ++u) {
+                    if (r + u < rows) {
 #pragma unroll
-                    for (int v = 0; v < kVecs; ++v) {
-                        const int i = base_slot + v * 256;
-                        x[u][v] = all ? *reinterpret_cast<const Four<W> *>(at + i) : load_four(at, i, columns);
+                        for (int v = 0; v < kVecs; ++v) {
+                            const int i = base_slot + v * 256;
+                            x[u][v] = all ? *reinterpret_cast<const Four<W> *>(at + i) : load_four(at, i, columns);
+                        }
+                        at += w.row_stride;
+                        if (++t == tokens) t = 0, at += gap;
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < kVecs; ++v) x[u][v] = {};
                     }
-                    at += w.row_stride;
-                    if (++t == tokens) t = 0, at += gap;
-                } else {
-#pragma unroll
-                    for (int v = 0; v < kVecs; ++v) x[u][v] = {};
                 }
+                if (look) {
+#pragma unroll
+                    for (int u = 0; u < kRows; ++u)
+#pragma unroll
+                        for (int e = 0; e < kEach; ++e) x[u][e >> 2].v[e & 3] = finite_or_none(x[u][e >> 2].v[e & 3]);
+                }
+#pragma unroll
+                for (int u = 0; u < kRows; ++u)
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) total[e] += (double)to_float(x[u][e >> 2].v[e & 3]);
             }
+            bool finite = true;
 #pragma unroll
-            for (int u = 0; u < kRows; ++u)
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) total[e] += as_weight(x[u][e >> 2].v[e & 3]);
+            for (int e = 0; e < kEach; ++e) finite &= is_finite(total[e]);
+            if (__ballot(!finite) == 0) break;
         }
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[v * 4 + j] = s[v].v[j] = (float)total[v * 4 + j];
+            for (int j = 0; j < 4; ++j) sum[v * 4 + j] = s[v].v[j] = (float)((double)s[v].v[j] + total[v * 4 + j]);
             take(v, s[v], p[v]);
         }
     } else {

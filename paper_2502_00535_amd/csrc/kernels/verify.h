@@ -62,7 +62,7 @@ struct Weights {
         double w = (double)as_probability(pj);
         if (kDraft && q != nullptr) {
             w -= (double)as_probability(qj);
-            w = w > 0.0 ? w : 0.0;
+            w = __builtin_fmax(w, 0.0);
         }
         return w;
     }

@@ -17,9 +17,8 @@
 #include "nms_pair.h"  // NMS_HD
 
 // ---- keys of the cache's order ----------------------------------------------------------------
-// A larger key stays longer; slots with equal keys stay in ascending order.  The bits are looked at, never compared as
-// floats, since device code is compiled without regard for NaN: sums that are not a number get the lowest key, and both
-// zeros the same one.  Protected rows lie above +infinity.
+// A larger key stays longer; slots with equal keys stay in ascending order.  Sums that are not a number get the lowest key,
+// and both zeros the same one.  Protected rows lie above +infinity.
 #define NMS_CACHE_KEY_PROTECTED 0xffffffffu
 NMS_HD uint32_t nms_cache_key_bits(uint32_t u)
 {
