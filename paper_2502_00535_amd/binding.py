@@ -572,17 +572,18 @@ NMS_MAX_FRAMES, NMS_MAX_DRAFTS, NMS_MAX_VOCABULARY, NMS_MAX_SLOTS, NMS_CACHE_MAX
 _TYPES = {torch.float32: NMS_TYPE_F32, torch.float16: NMS_TYPE_F16, torch.bfloat16: NMS_TYPE_BF16}
 
 
-def _here(**tensors):
-    """The kernels run on the current device: tensors of another one are refused."""
-    for what, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
-            raise ValueError(f"{what}: tensor lives on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+def _here(*named):
+    """The kernels run on the current device: tensors of another one are refused.  (name, tensor) in turn."""
+    device = torch.cuda.current_device()
+    for what, t in zip(named[::2], named[1::2]):
+        if isinstance(t, _Tensor) and t.is_cuda and t.get_device() != device:
+            raise ValueError(f"{what}: tensor lives on {t.device}, the current device is cuda:{device}")
 
 
 def _strided(t, what):
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{what}: expected a torch tensor")
-    if not _on_device(t):
+    if not t.is_cuda:
         raise ValueError(f"{what}: tensor must live on the GPU")
     return t
 
@@ -596,18 +597,21 @@ def _type_of(t, what):
 def _rows(t, shape, what):
     """(address, stride from row to row) of a tensor whose leading dimensions are `shape` but the last, and whose last holds at least
     shape[-1] neighbouring elements: rows may lie apart, all at one distance."""
-    t = _strided(t, what)
-    if t.dim() != len(shape) or tuple(t.shape[:-1]) != tuple(shape[:-1]) or t.shape[-1] < shape[-1]:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, the call needs {tuple(shape)}")
-    if shape[-1] > 1 and t.stride(-1) != 1:
+    has = tuple(_strided(t, what).shape)
+    if has == shape and t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    if len(has) != len(shape) or has[:-1] != shape[:-1] or has[-1] < shape[-1]:
+        raise ValueError(f"{what}: shape {has}, the call needs {shape}")
+    strides = t.stride()
+    if shape[-1] > 1 and strides[-1] != 1:
         raise ValueError(f"{what}: the elements of a row must be neighbours")
     row, expect = None, None
     for d in range(len(shape) - 2, -1, -1):
         if shape[d] == 1:
             continue
         if row is None:
-            row = expect = t.stride(d)
-        if t.stride(d) != expect:
+            row = expect = strides[d]
+        if strides[d] != expect:
             raise ValueError(f"{what}: rows must lie at one distance from each other")
         expect *= shape[d]
     if row is None:
@@ -623,8 +627,8 @@ def nms_verify_workspace_bytes(vocabulary: int, sequences: int) -> int:
 
 def _verify_arguments(target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace):
     k, v, s = int(drafts_max), int(vocabulary), int(sequences)
-    _here(target=target, draft=draft, drafts=drafts, counts=counts, uniforms=uniforms, tokens_out=tokens_out,
-          accepted_out=accepted_out, workspace=workspace)
+    _here("target", target, "draft", draft, "drafts", drafts, "counts", counts, "uniforms", uniforms, "tokens_out", tokens_out,
+          "accepted_out", accepted_out, "workspace", workspace)
     t_at, t_row, d_at, d_row, kind = None, v, None, v, NMS_TYPE_F32
     if 0 <= k <= NMS_MAX_DRAFTS and 1 <= v <= NMS_MAX_VOCABULARY and 1 <= s <= NMS_MAX_FRAMES:  # else the library refuses the sizes, or there is nothing to do
         t_at, t_row = _rows(target, (s, k + 1, v), "target")
@@ -667,50 +671,55 @@ def _cache_weights(weights, valid_tokens, heads, sequences):
     """struct nms_cache_weights of a tensor [sequences, heads, group, tokens, columns], or None."""
     if weights is None:
         return None
-    weights = _strided(weights, "weights")
-    if weights.dim() != 5 or weights.shape[0] != sequences or weights.shape[1] != heads:
-        raise ValueError(f"weights: shape {tuple(weights.shape)}, the call needs ({sequences}, {heads}, group, tokens, columns)")
-    at, row = _rows(weights, tuple(weights.shape), "weights")
-    return NmsCacheWeights(at, row, _type_of(weights, "weights"), weights.shape[2], weights.shape[3], weights.shape[4],
+    shape = tuple(_strided(weights, "weights").shape)
+    if len(shape) != 5 or shape[0] != sequences or shape[1] != heads:
+        raise ValueError(f"weights: shape {shape}, the call needs ({sequences}, {heads}, group, tokens, columns)")
+    at, row = _rows(weights, shape, "weights")
+    return NmsCacheWeights(at, row, _type_of(weights, "weights"), shape[2], shape[3], shape[4],
                            _ptr(valid_tokens, "int32", "valid_tokens", sequences))
 
 
-def _cache_tensors(tensors, n_max, heads, sequences, page_table):
-    """Array of struct nms_cache_tensor, and struct nms_cache_pages or None."""
-    tensors = list(tensors or ())
-    structs, shape = (NmsCacheTensor * max(len(tensors), 1))(), None
-    for i, t in enumerate(tensors):
-        what = f"tensors[{i}]"
-        t = _strided(t, what)
-        if t.dim() < 3 or t.shape[1] < heads or (page_table is None and (t.shape[0] < sequences or t.shape[2] < n_max)):
-            need = f"({sequences}, {heads}, {n_max}, ...)" if page_table is None else f"(pages, {heads}, slots of a page, ...)"
-            raise ValueError(f"{what}: shape {tuple(t.shape)}, the call needs {need}")
-        row = 1
-        for d in range(t.dim() - 1, 2, -1):
-            if t.shape[d] != 1 and t.stride(d) != row:
-                raise ValueError(f"{what}: the elements of a row must be neighbours")
-            row *= t.shape[d]
+def _cache_tensor(t, what, n_max, heads, sequences, paged):
+    """The fields of struct nms_cache_tensor for a tensor whose rows are whole and lie apart."""
+    shape = tuple(_strided(t, what).shape)
+    if len(shape) < 3 or shape[1] < heads or (not paged and (shape[0] < sequences or shape[2] < n_max)):
+        need = f"({sequences}, {heads}, {n_max}, ...)" if not paged else f"(pages, {heads}, slots of a page, ...)"
+        raise ValueError(f"{what}: shape {shape}, the call needs {need}")
+    strides, row = t.stride(), 1
+    for d in range(len(shape) - 1, 2, -1):
+        if shape[d] != 1 and strides[d] != row:
+            raise ValueError(f"{what}: the elements of a row must be neighbours")
+        row *= shape[d]
+    if not t.is_contiguous():
         extent = row
-        for stride, size in sorted((t.stride(d), t.shape[d]) for d in range(3)):
+        for stride, size in sorted(zip(strides[:3], shape[:3])):
             if size > 1:
                 if stride < extent:
                     raise ValueError(f"{what}: rows must not overlap")
                 extent += stride * (size - 1)
-        if shape is None:
-            shape = (t.shape[0], t.shape[2])
-        elif page_table is not None and shape != (t.shape[0], t.shape[2]):
-            raise ValueError(f"{what}: pages of the tensors must be as many and as long")
-        b = t.element_size()
-        structs[i] = NmsCacheTensor(t.data_ptr(), row * b, t.stride(0) * b, t.stride(1) * b, t.stride(2) * b)
-    if page_table is None or not tensors:
+    b = t.element_size()
+    return t.data_ptr(), row * b, strides[0] * b, strides[1] * b, strides[2] * b
+
+
+def _cache_tensors(tensors, n_max, heads, sequences, page_table):
+    """Array of struct nms_cache_tensor, its length, and struct nms_cache_pages or None."""
+    tensors = list(tensors or ())
+    if not tensors:
+        return None, 0, None
+    structs = (NmsCacheTensor * len(tensors))(*[_cache_tensor(t, f"tensors[{i}]", n_max, heads, sequences, page_table is not None)
+                                                for i, t in enumerate(tensors)])
+    if page_table is None:
         return structs, len(tensors), None
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] < sequences:
+    count, slots = tensors[0].shape[0], tensors[0].shape[2]
+    for i, t in enumerate(tensors):
+        if t.shape[0] != count or t.shape[2] != slots:
+            raise ValueError(f"tensors[{i}]: pages of the tensors must be as many and as long")
+    if not isinstance(page_table, _Tensor) or page_table.dim() != 2 or page_table.shape[0] < sequences:
         raise ValueError(f"page_table: expected a tensor ({sequences}, pages of a sequence)")
-    each = -(-max(n_max, 0) // max(shape[1], 1))
+    each = -(-max(n_max, 0) // max(slots, 1))
     if page_table.shape[1] < each:
         raise ValueError(f"page_table: {page_table.shape[1]} pages to a sequence, the call needs {each}")
-    at = _ptr(page_table, "int32", "page_table", 0)
-    return structs, len(tensors), NmsCachePages(at, page_table.shape[1], shape[1], shape[0], 0)
+    return structs, len(tensors), NmsCachePages(_ptr(page_table, "int32", "page_table", 0), page_table.shape[1], slots, count, 0)
 
 
 def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, keep_out, kept_out, moves_out,
@@ -718,8 +727,8 @@ def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, seque
     """weights: [sequences, heads, group, tokens, columns], rows at one distance from each other, or None.
     moves_out: at least sequences * heads * (nms_cache_moves_max(n_max, budget) + 1) * 2 elements, or None."""
     n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
-    _here(sums=sums, positions=positions, counts=counts, lengths=lengths, keep_out=keep_out, kept_out=kept_out, moves_out=moves_out,
-          workspace=workspace, weights=weights, valid_tokens=valid_tokens)
+    _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
+          "moves_out", moves_out, "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens)
     all_, s_ = _cache_elements(n, h, s)
     w, wb = _ws(workspace)
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
@@ -735,7 +744,7 @@ def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page
     """tensors: up to eight of shape [sequences, heads, n_max, row ...] (any strides whose rows are whole), or with a page table
     ([sequences, pages of a sequence] int32) [pages, heads, slots of a page, row ...]."""
     n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
-    _here(moves=moves, page_table=page_table, **{f"tensors[{i}]": t for i, t in enumerate(tensors or ())})
+    _here("moves", moves, "page_table", page_table, *(x for t in tensors or () for x in ("tensors", t)))
     all_, s_ = _cache_elements(n, h, s)
     structs, many, pages = _cache_tensors(tensors, n, h, s, page_table)
     _check(lib.nms_cache_move_batched(_ptr(moves, "int32", "moves", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ else 0),
@@ -745,8 +754,9 @@ def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page
 def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
                      workspace, weights, valid_tokens, page_table):
     n, h, s = int(n_max), int(heads), int(sequences)
-    _here(sums=sums, positions=positions, counts=counts, lengths=lengths, keep_out=keep_out, kept_out=kept_out, workspace=workspace,
-          weights=weights, valid_tokens=valid_tokens, page_table=page_table, **{f"tensors[{i}]": t for i, t in enumerate(tensors or ())})
+    _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
+          "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens, "page_table", page_table,
+          *(x for t in tensors or () for x in ("tensors", t)))
     all_, s_ = _cache_elements(n, h, s)
     w, wb = _ws(workspace)
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None

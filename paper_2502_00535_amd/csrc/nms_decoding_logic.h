@@ -2,7 +2,10 @@
 #define NMS_SPLIT (n_max > 32768 || (n_max > 16384 && frames <= 32))
 #endif
 #ifndef NMS_FUSE
-#define NMS_FUSE (rows <= 32)
+#define NMS_FUSE (rows <= 8 || (rows <= 16 && frames >= 1024))
+#endif
+#ifndef NMS_V1
+#define NMS_V1 1024
 #endif
 // Host-checkable logic of the decoding step's choices (verification of drafted tokens, eviction from a cache): keys,
 // sizes, workspace layout and addresses.  Compiled by hipcc for the library and by a plain host compiler for the tests.
@@ -46,7 +49,7 @@ static inline bool nms_cache_split(int n_max, int frames) { return NMS_SPLIT; }
 // Else: vectors of four slots to a lane, a frame is one workgroup of at most sixteen wavefronts.
 static inline int nms_cache_vecs(int n_max)
 {
-    int vecs = n_max <= 1024 ? 1 : 2;
+    int vecs = n_max <= NMS_V1 ? 1 : 2;
     while (n_max > 16 * 256 * vecs) vecs *= 2;
     return vecs;
 }

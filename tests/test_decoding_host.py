@@ -148,6 +148,9 @@ class OnGpu(torch.Tensor):
     def device(self):
         return torch.device("cuda", 0)
 
+    def get_device(self):
+        return 0
+
 
 def gpu(*shape, dtype=torch.float32):
     return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
