@@ -427,7 +427,8 @@ int nms_verify_batched(const void *target, long long target_stride, const void *
  *   weights    HOST pointer, or NULL (nothing is added)
  *   keep_out   [sequences][heads][n_max] bytes, 1 = the row of this slot stays (slots as before any move), 0 = it goes or
  *              there is none; NULL: not wanted
- *   kept_out   [sequences] int32, k: the next step's rows are written behind it (a buffer other than counts); NULL: not wanted
+ *   kept_out   [sequences] int32, k: the next step's rows are written behind it (a buffer other than counts, lengths and
+ *              valid_tokens: else NMS_ERR_INVALID_ARG); NULL: not wanted
  *   moves_out  int32 [sequences][heads][nms_cache_moves_max(n_max, budget) + 1][2]: the number of moves and 0, then pairs
  *              (to, from), to ascending, from ascending; entries behind them are left as they are; NULL: not wanted
  *   workspace  >= nms_cache_workspace_bytes(n_max, heads, sequences, budget) bytes, 256-byte aligned

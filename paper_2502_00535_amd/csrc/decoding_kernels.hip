@@ -83,6 +83,12 @@ int weights_status(const nms_cache_weights *w)
     return NMS_OK;
 }
 
+// kept_out is written while other workgroups still read these.
+bool overwrites(const int32_t *kept, const int32_t *counts, const int32_t *lengths, const nms_cache_weights *w)
+{
+    return kept != nullptr && (kept == counts || kept == lengths || (w != nullptr && kept == w->valid_tokens));
+}
+
 int tensors_status(const nms_cache_tensor *tensors, int n_tensors, const nms_cache_pages *pages, int n_max)
 {
     if (n_tensors < 0 || (n_tensors > 0 && tensors == nullptr)) return NMS_ERR_INVALID_ARG;
@@ -194,7 +200,7 @@ int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const Mo
     if (few && a.move_sums) b.moves = nullptr;  // the list stays in LDS
     const MoveArgs none = {}, &now = few ? m : none;
     int st;
-    switch (nms_cache_vecs(a.n_max)) {
+    switch (nms_cache_vecs(a.n_max, frames)) {
     case 1: st = keep_launch<1>(b, w, type, now, frames, stream); break;
     case 2: st = keep_launch<2>(b, w, type, now, frames, stream); break;
     case 4: st = keep_launch<4>(b, w, type, now, frames, stream); break;
@@ -256,7 +262,7 @@ int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t 
     st = weights_status(weights);
     if (st != NMS_OK) return st;
     if (n_max == 0 || heads == 0 || sequences == 0) return NMS_OK;
-    if (sums == nullptr) return NMS_ERR_INVALID_ARG;
+    if (sums == nullptr || overwrites(kept_out, counts, lengths, weights)) return NMS_ERR_INVALID_ARG;
     st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
     if (st != NMS_OK) return st;
     const CacheArgs a = {sums, const_cast<int32_t *>(positions), counts, lengths, keep_out, kept_out, moves_out, n_max, heads, budget, first, recent,
@@ -289,7 +295,7 @@ int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *coun
     st = tensors_status(tensors, n_tensors, pages, n_max);
     if (st != NMS_OK) return st;
     if (n_max == 0 || heads == 0 || sequences == 0) return NMS_OK;
-    if (sums == nullptr) return NMS_ERR_INVALID_ARG;
+    if (sums == nullptr || overwrites(kept_out, counts, lengths, weights)) return NMS_ERR_INVALID_ARG;
     st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
     if (st != NMS_OK) return st;
     const int frames = heads * sequences;

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, 
 
 // A lane has kVecs times four neighbouring slots, a wavefront 256 * kVecs neighbouring ones, so that the rank of a slot among others is a
 // count over the wavefronts before, the vectors before, the lanes before and the lane's own.
-constexpr int kKeepMaxWaves = 16;
+constexpr int kKeepMaxWaves = NMS_CACHE_WAVES;
 constexpr int kKeepBins = kKeepMaxWaves * 64 * 2;  // two to a thread
 constexpr int kFew = 64;                           // candidates that are compared one with another; moves that need no list in memory
 
@@ -181,7 +181,7 @@ struct KeepRoom {
     uint32_t few, few_keys[kFew];
 };
 
-// Where the best `need` of the `left` keys between lo and hi end (0 < need <= left): at the least that stays, and how many keys equal to it are
+// Where the best `need` of the `left` keys between lo and hi end (0 < need <= left; exact: lo is one of them): at the least that stays, and how many keys equal to it are
 // wanted and there.
 struct Cut {
     uint32_t key, wanted, there;
@@ -193,9 +193,20 @@ struct Cut {
 // there) they are added as one.
 template <int kVecs>
 __device__ __forceinline__ Cut find_cut(KeepRoom &room, const uint32_t (&key)[kVecs * 4], uint32_t lo, uint32_t hi, uint32_t need, uint32_t left,
-                                        int wave, int lane)
+                                        bool exact, int wave, int lane)
 {
     const int log_bins = 31 - __builtin_clz(blockDim.x * 2);
+    if (left - need == 1 && exact) {  // one goes, as in a decoding step of one token: the smallest key, if no other is the same
+        uint32_t equal = 0;
+#pragma unroll
+        for (int e = 0; e < kVecs * 4; ++e) equal += __popcll(__ballot(key[e] == lo));
+        if (lane == 0) room.wave_c[wave] = equal;
+        __syncthreads();
+        equal = 0;
+        for (int i = 0; i < (int)(blockDim.x >> 6); ++i) equal += room.wave_c[i];
+        __syncthreads();
+        return equal == 1 ? Cut{lo + 1, 0u, 0u} : Cut{lo, equal - 1, equal};
+    }
     for (;;) {
         if (left == need) return {lo, 0u, 0u};    // all that are left: whatever lies at or beyond lo
         if (lo == hi) return {lo, need, left};
@@ -283,28 +294,27 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     const int newest = since < INT32_MIN ? INT32_MIN : (int)since;
     const int base_slot = wave * (256 * kVecs) + lane * 4;
     auto slot_of = [&](int e) { return base_slot + (e >> 2) * 256 + (e & 3); };
-    const bool whole = (wave + 1) * (256 * kVecs) <= n;  // of the wavefront: every slot holds a row
     uint32_t key[kEach], largest = 0, smallest = 0, guarded = 0;  // smallest: as its complement; both without the protected rows
-    auto take = [&](int v, const Four<float> &s, const Four<int32_t> &p) {
+    auto take = [&](auto whole, int v, const Four<float> &s, const Four<int32_t> &p) {  // whole: every slot of the wavefront holds a row
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            const bool there = decltype(whole)::value || base_slot + v * 256 + j < n;
             const bool protect = p.v[j] < a.first || p.v[j] >= newest;
-            const uint32_t u = live_key(s.v[j], protect);
-            const bool there = whole || base_slot + v * 256 + j < n;
-            key[v * 4 + j] = there ? u : 0u;
-            largest = max(largest, there && !protect ? u : 0u);
-            smallest = max(smallest, there && !protect ? ~u : 0u);
-            guarded += there && protect;
+            const uint32_t u = there ? live_key(s.v[j], protect) : 0u, among = protect ? 0u : u;
+            key[v * 4 + j] = u;
+            largest = max(largest, among);
+            smallest = max(smallest, among != 0u ? ~u : 0u);
+            guarded += u == NMS_CACHE_KEY_PROTECTED;
         }
     };
-    auto places = [&](int v) {
+    auto places = [&](auto whole, int v) {
         const int i = base_slot + v * 256;
         if (a.positions == nullptr) return Four<int32_t>{{i, i + 1, i + 2, i + 3}};
-        return whole ? *reinterpret_cast<const Four<int32_t> *>(a.positions + base + i) : load_four(a.positions + base, i, n);
+        return decltype(whole)::value ? *reinterpret_cast<const Four<int32_t> *>(a.positions + base + i) : load_four(a.positions + base, i, n);
     };
-    auto sums_of = [&](int v) {
+    auto sums_of = [&](auto whole, int v) {
         const int i = base_slot + v * 256;
-        return whole ? *reinterpret_cast<const Four<float> *>(a.sums + base + i) : load_four(a.sums + base, i, n);
+        return decltype(whole)::value ? *reinterpret_cast<const Four<float> *>(a.sums + base + i) : load_four(a.sums + base, i, n);
     };
     float sum[kWeights ? kEach : 1];  // with weights: the new sums, in memory only once their places are known
     if constexpr (kWeights) {
@@ -317,9 +327,9 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         Four<float> s[kVecs];
         double total[kEach];
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) s[v] = sums_of(v);
+        for (int v = 0; v < kVecs; ++v) s[v] = sums_of(std::false_type{}, v);
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) p[v] = places(v);
+        for (int v = 0; v < kVecs; ++v) p[v] = places(std::false_type{}, v);
         for (bool look : {false, true}) {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) total[e] = 0.0;
@@ -361,21 +371,25 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[v * 4 + j] = s[v].v[j] = (float)((double)s[v].v[j] + total[v * 4 + j]);
-            take(v, s[v], p[v]);
+            take(std::false_type{}, v, s[v], p[v]);
         }
     } else {
         constexpr int kAtOnce = kVecs < 4 ? kVecs : 4;
+        auto load = [&](auto whole) {
 #pragma unroll
-        for (int v0 = 0; v0 < kVecs; v0 += kAtOnce) {
-            Four<int32_t> p[kAtOnce];
-            Four<float> s[kAtOnce];
+            for (int v0 = 0; v0 < kVecs; v0 += kAtOnce) {
+                Four<int32_t> p[kAtOnce];
+                Four<float> s[kAtOnce];
 #pragma unroll
-            for (int v = 0; v < kAtOnce; ++v) s[v] = sums_of(v0 + v);
+                for (int v = 0; v < kAtOnce; ++v) s[v] = sums_of(whole, v0 + v);
 #pragma unroll
-            for (int v = 0; v < kAtOnce; ++v) p[v] = places(v0 + v);
+                for (int v = 0; v < kAtOnce; ++v) p[v] = places(whole, v0 + v);
 #pragma unroll
-            for (int v = 0; v < kAtOnce; ++v) take(v0 + v, s[v], p[v]);
-        }
+                for (int v = 0; v < kAtOnce; ++v) take(whole, v0 + v, s[v], p[v]);
+            }
+        };
+        if ((wave + 1) * (256 * kVecs) <= n) load(std::true_type{});
+        else load(std::false_type{});
     }
     // which rows stay, a bit to an element
     using Bits = typename std::conditional<(kEach > 32), unsigned long long, uint32_t>::type;
@@ -399,8 +413,8 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         uint32_t lo = ~smallest, hi = largest, need = (uint32_t)k - guarded, left = (uint32_t)n - guarded;
         if ((uint32_t)k <= guarded) lo = hi = NMS_CACHE_KEY_PROTECTED, need = (uint32_t)k, left = guarded;  // protected rows alone
         Cut cut;
-        for (;;) {
-            cut = find_cut<kVecs>(room, key, lo, hi, need, left, wave, lane);
+        for (bool exact = true;; exact = false) {
+            cut = find_cut<kVecs>(room, key, lo, hi, need, left, exact, wave, lane);
             const bool ties = cut.wanted < cut.there;
 #pragma unroll
             for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] > cut.key || (key[e] == cut.key && !ties)) << e;

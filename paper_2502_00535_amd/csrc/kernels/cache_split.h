@@ -143,13 +143,23 @@ __global__ void __launch_bounds__(kCutThreads) cache_split_cut_kernel(CacheArgs 
         hi = bin == kSplitBins - 1 ? ~0ull : (unsigned long long)(kSplitBase + ((bin + 1) << kSplitShift)) << 32;
         if (bin != kSplitBins - 1) --hi;
     }
-    bool listed = false;  // the rows between lo and hi are in LDS
+    const uint32_t first_bin = found[0];
+    bool listed = false, recounted = false;  // the rows between lo and hi are in LDS; they were counted again from memory
     uint32_t entries = 0;
+    // the rows between lo and hi; in memory their keys are looked at first, in 32 bits, since hardly any passes (one compute unit looks at all of them)
     auto for_rows = [&](auto &&visit) {
         if (listed) {
-            for (uint32_t i = threadIdx.x; i < entries; i += kCutThreads) visit(list[i]);
+            for (uint32_t i = threadIdx.x; i < entries; i += kCutThreads)
+                if (list[i] - lo <= hi - lo) visit(list[i]);
         } else {
-            constexpr int kAtOnce = 4, kStep = kCutThreads * 4;
+            constexpr int kAtOnce = 8, kStep = kCutThreads * 4;
+            const uint32_t least = (uint32_t)(lo >> 32), range = (uint32_t)(hi >> 32) - least;
+            auto look = [&](uint32_t key, int i) {
+                if (key - least <= range) {
+                    const unsigned long long v = row(key, i);
+                    if (v - lo <= hi - lo) visit(v);
+                }
+            };
             int i = threadIdx.x * 4;
             for (; i - (int)threadIdx.x * 4 + kAtOnce * kStep <= n; i += kAtOnce * kStep) {
                 Four<uint32_t> u[kAtOnce];
@@ -158,13 +168,13 @@ __global__ void __launch_bounds__(kCutThreads) cache_split_cut_kernel(CacheArgs 
 #pragma unroll
                 for (int c = 0; c < kAtOnce; ++c)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) visit(row(u[c].v[j], i + c * kStep + j));
+                    for (int j = 0; j < 4; ++j) look(u[c].v[j], i + c * kStep + j);
             }
             for (; i < n; i += kStep) {
                 const Four<uint32_t> u = load_four(keys, i, n);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (i + j < n) visit(row(u.v[j], i + j));
+                    if (i + j < n) look(u.v[j], i + j);
             }
         }
     };
@@ -172,20 +182,17 @@ __global__ void __launch_bounds__(kCutThreads) cache_split_cut_kernel(CacheArgs 
         if (!listed && left <= (uint32_t)kSplitList) {
             if (threadIdx.x == 0) few = 0;
             __syncthreads();
-            for_rows([&](unsigned long long v) {
-                if (v >= lo && v <= hi) list[atomicAdd(&few, 1u) & (kSplitList - 1)] = v;
-            });
+            for_rows([&](unsigned long long v) { list[atomicAdd(&few, 1u) & (kSplitList - 1)] = v; });
             __syncthreads();
             listed = true;
             entries = left;
         }
         const unsigned long long range = hi - lo;  // not 0: the rows differ
         const int bits = 64 - __builtin_clzll(range), shift = bits > 11 ? bits - 11 : 0;
+        recounted |= !listed;
         bins[threadIdx.x] = bins[kCutThreads + threadIdx.x] = 0;
         __syncthreads();
-        for_rows([&](unsigned long long v) {
-            if (v - lo <= range) atomicAdd(&bins[(v - lo) >> shift], 1u);
-        });
+        for_rows([&](unsigned long long v) { atomicAdd(&bins[(v - lo) >> shift], 1u); });
         __syncthreads();
         b0 = bins[2 * threadIdx.x], b1 = bins[2 * threadIdx.x + 1];
         const uint32_t bin = choose();
@@ -195,26 +202,49 @@ __global__ void __launch_bounds__(kCutThreads) cache_split_cut_kernel(CacheArgs 
         if (shift == 0) break;  // one row
     }
     if (threadIdx.x == 0) x.cuts[frame] = lo;
+    // how many rows of each part stay: those of larger bins by the part's counts, and those of the cut's bin (all, or by the list)
+    uint32_t *stays = x.stays + (long long)frame * x.parts;
+    if (!recounted) {
+        __syncthreads();
+        for (int p = threadIdx.x; p < parts; p += kCutThreads) bins[p] = 0;
+        __syncthreads();
+        if (listed) {
+            const int low = (k + x.part - 1) / x.part;
+            for (uint32_t i = threadIdx.x; i < entries; i += kCutThreads) {
+                const int slot = (int)~(uint32_t)list[i];
+                if (list[i] >= lo) atomicAdd(&bins[slot < k ? slot / x.part : low + (slot - k) / x.part], 1u);
+            }
+        }
+        __syncthreads();
+        const uint32_t least = listed ? first_bin + 1 : first_bin;
+        for (int p = wave; p < parts; p += kCutWaves) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(x.bins + ((long long)frame * x.parts + p) * kSplitBins);
+            uint32_t c = 0;
+#pragma unroll
+            for (int v = 0; v < kSplitBins / 8 / 64; ++v) {
+                const uint4 u = from[v * 64 + lane];
+                const uint32_t pair[4] = {u.x, u.y, u.z, u.w}, bin = (v * 64 + lane) * 8;
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    c += bin + 2 * j >= least ? pair[j] & 0xffffu : 0u;
+                    c += bin + 2 * j + 1 >= least ? pair[j] >> 16 : 0u;
+                }
+            }
+            c = of_lane(wave_running_count(c), 63);
+            if (lane == 0) stays[p] = c + bins[p];
+        }
+        return;
+    }
     for (int p = wave; p < parts; p += kCutWaves) {
         const int2 r = split_range(p, n, k, x.part);
         uint32_t c = 0;
-        int i0 = r.x;
-        for (; i0 + 1024 <= r.y; i0 += 1024) {
-            Four<uint32_t> u[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) u[v] = *reinterpret_cast<const Four<uint32_t> *>(keys + i0 + v * 256 + lane * 4);
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c += row(u[v].v[j], i0 + v * 256 + lane * 4 + j) >= lo;
-        }
-        for (int i = i0 + lane * 4; i < r.y; i += 256) {
+        for (int i = r.x + lane * 4; i < r.y; i += 256) {
             const Four<uint32_t> u = load_four(keys, i, r.y);
 #pragma unroll
             for (int j = 0; j < 4; ++j) c += i + j < r.y && row(u.v[j], i + j) >= lo;
         }
         c = of_lane(wave_running_count(c), 63);
-        if (lane == 0) x.stays[(long long)frame * x.parts + p] = c;
+        if (lane == 0) stays[p] = c;
     }
 }
 

@@ -1,12 +1,3 @@
-#ifndef NMS_SPLIT
-#define NMS_SPLIT (n_max > 32768 || (n_max > 16384 && frames <= 32))
-#endif
-#ifndef NMS_FUSE
-#define NMS_FUSE (rows <= 8 || (rows <= 16 && frames >= 1024))
-#endif
-#ifndef NMS_V1
-#define NMS_V1 1024
-#endif
 // Host-checkable logic of the decoding step's choices (verification of drafted tokens, eviction from a cache): keys,
 // sizes, workspace layout and addresses.  Compiled by hipcc for the library and by a plain host compiler for the tests.
 #ifndef NMS_DECODING_LOGIC_H
@@ -44,19 +35,27 @@ NMS_HD int nms_moves_max(int n_max, int budget)
 }
 static inline size_t nms_decoding_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // ---- eviction: the route ------------------------------------------------------------------------
-// Frames longer than a workgroup's registers hold are shared by several workgroups, in three launches.
-static inline bool nms_cache_split(int n_max, int frames) { return NMS_SPLIT; }
-// Else: vectors of four slots to a lane, a frame is one workgroup of at most sixteen wavefronts.
-static inline int nms_cache_vecs(int n_max)
+// A frame is one workgroup with the keys of all its slots in registers, or (split) is shared by several workgroups in three launches: frames that
+// registers do not hold, and long ones of small batches.  Keep vector alone, us, one workgroup / split: 8 x 16,384 slots 11.6 / 16.0; 8 x 32,768
+// 17.8 / 17.9; 64 x 32,768 20.3 / 24.2; 512 x 32,768 50 / 76.  Whole path with 64 query rows: 8 x 16,384 35.6 / 35.6; 32 x 32,768 91 / 82.
+#define NMS_CACHE_WAVES 16   // most wavefronts to a workgroup
+static inline bool nms_cache_split(int n_max, int frames) { return n_max > 32768 || (n_max > 16384 && frames <= 32); }
+// Vectors of four slots to a lane: one while sixteen wavefronts reach and the batch's wavefronts are on the chip at once, two or more otherwise.  A step
+// of one token, us, one vector / two (bf16 weights): 8 heads x 2001 slots 9.1 / 10.7; 8 x 3501 10.3 / 10.6; 512 x 2001 11.6 / 12.5; 1024 x 1501
+// (6144 wavefronts) 13.2 / 13.7; 512 x 3501 (7168) 20.0 / 14.5; 1024 x 2501 28.1 / 18.2; 2048 x 1501 27.3 / 20.0.
+static inline int nms_cache_vecs(int n_max, int frames)
 {
-    int vecs = n_max <= NMS_V1 ? 1 : 2;
-    while (n_max > 16 * 256 * vecs) vecs *= 2;
+    if (n_max <= 1024 || (n_max <= 3584 && (long long)frames * ((n_max + 255) / 256) <= 6144)) return 1;
+    int vecs = 2;
+    while (n_max > NMS_CACHE_WAVES * 256 * vecs) vecs *= 2;
     return vecs;
 }
-// The weights are added by the launch that finds the rows that stay where there are few query rows, by one of its own otherwise.
+// The weights are added by the launch that finds the rows that stay where there are few query rows, by one of its own otherwise.  Whole call, us, with it /
+// on their own (bf16): 4 query rows, 8 x 4001 11.5 / 12.6, 512 x 2001 12.2 / 20.3; 16, 8 x 4001 16.9 / 13.2, 256 x 4001 23.4 / 23.9, 1024 x 1001 18.5 / 23.5;
+// 32, 8 x 4001 24.1 / 14.1, 256 x 4001 36.8 / 30.6, 1024 x 1001 27.8 / 29.7.
 static inline bool nms_cache_add_with_keep(int n_max, int frames, long long rows)
 {
-    return !nms_cache_split(n_max, frames) && NMS_FUSE && nms_cache_vecs(n_max) <= 4;
+    return !nms_cache_split(n_max, frames) && nms_cache_vecs(n_max, frames) <= 4 && (rows <= 8 || (rows <= 16 && frames >= 1024));
 }
 
 // Scratch: the list of moves (of the whole path), and what the three launches hand on.

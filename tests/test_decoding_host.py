@@ -62,6 +62,35 @@ def test_moves_and_scratch(driver, nms):
     assert nms.nms_verify_workspace_bytes(0, 1) == 0 and nms.nms_verify_workspace_bytes(4194305, 1) == 0 and nms.nms_verify_workspace_bytes(5, 65536) == 0
 
 
+def test_routes_of_eviction_fit_their_kernels(driver):
+    """One workgroup: at most sixteen wavefronts whose lanes hold every slot, 16-bit slot numbers, the lists within 160 KiB of LDS.  Several: parts that
+    cover the frame with one to spare, 16-bit counts, a list of parts within the cut's LDS, and scratch without overlaps."""
+    sizes = sorted({1, 2, 255, 256, 1023, 1024, 1025, 2048, 3583, 3584, 3585, 4096, 4097, 8192, 8193, 16384, 16385, 32768, 32769, 65536, 100003, 524288, 1048575, 1048576})
+    cases = [(n, f, r) for n in sizes for f in (1, 8, 32, 33, 300, 512, 1024, 65535) for r in (1, 8, 9, 16, 17)]
+    for (n, f, rows), line in zip(cases, driver("route", [" ".join(map(str, c)) for c in cases])):
+        split, vecs, together, part, parts, keys, bins, cuts, stays, total = (int(x) for x in line.split())
+        if not split:
+            waves = -(-n // (256 * vecs))
+            assert vecs in (1, 2, 4, 8) and 1 <= waves <= 16 and n <= 65536
+            most_moves = n // 2
+            assert 8192 + 1024 + most_moves * (8 if together else 4) <= 160 * 1024
+            assert not together or vecs <= 4
+        else:
+            assert not together
+        assert part in (1024, 2048, 4096) and (parts - 1) * part >= n and parts <= 2048
+        assert bins - keys >= 4 * n * f and cuts - bins >= f * parts * 4096 and stays - cuts >= 8 * f and total - stays >= 4 * f * parts
+        assert all(x % 256 == 0 for x in (keys, bins, cuts, stays, total))
+
+
+def test_routes_of_verification(driver, nms):
+    cases = [(v, s) for v in (1, 2048, 2049, 40960, 40961, 131072, 4194304) for s in (1, 127, 128, 65535)]
+    for (v, s), line in zip(cases, driver("verify", [f"{v} {s}" for v, s in cases])):
+        segments, one, sums, scratch = (int(x) for x in line.split())
+        assert segments == -(-v // 2048) <= 2048 and one == (segments <= 20 or s >= 128)
+        assert scratch == nms.nms_verify_workspace_bytes(v, s) and (scratch == 0) == one
+        assert one or (sums >= 8 * segments * s and scratch - sums >= 8 * s and sums % 256 == 0)
+
+
 def test_pieces_divide_every_address(driver):
     cases = [(4096, 256, 1 << 20, 4096, 256, 16), (4096, 80, 8000, 800, 80, 16), (4096, 84, 8400, 840, 84, 4), (4104, 256, 4096, 512, 256, 8),
              (4097, 256, 4096, 512, 256, 1), (4096, 7, 70, 7, 7, 1), (4096, 20, 4000, 200, 20, 4), (4096, 10, 100, 20, 10, 2), (4096, 64, 0, 0, 64, 16)]
@@ -122,6 +151,9 @@ def test_refusals_of_eviction(nms):
         assert evict(**wrong) == bad and keep(**wrong) == bad, wrong
     for wrong in (dict(n=1048577), dict(h=65536, s=1), dict(h=300, s=300), dict(h=2147483647, s=2147483647)):
         assert evict(**wrong) == large and keep(**wrong) == large and move(**wrong) == large, wrong
+    for counts, lengths, w in ((p, None, None), (None, p, None), (None, None, nms.NmsCacheWeights(0x2000, 50, 0, 1, 1, 50, 0x1000))):  # kept_out is one of them
+        assert L.nms_cache_evict_batched(p, p, counts, lengths, 50, 2, 3, w, 10, 0, 4, tensor, 1, None, None, p, p, 1 << 40, None) == bad
+        assert L.nms_cache_keep_batched(p, p, counts, lengths, 50, 2, 3, w, 10, 0, 4, None, p, None, p, 1 << 40, None) == bad
     assert evict(positions=None) == bad                               # a window by places that nobody keeps
     for t in (nms.NmsCacheTensor(None, 16, 0, 0, 0), nms.NmsCacheTensor(0x1000, 0, 0, 0, 0), nms.NmsCacheTensor(0x1000, -5, 0, 0, 0),
               nms.NmsCacheTensor(0x1000, (1 << 20) + 1, 0, 0, 0)):

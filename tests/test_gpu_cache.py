@@ -150,6 +150,27 @@ def test_ties_everywhere(nms, s, h, n, budget, sums):
     Cache(nms, s, h, n, budget, sums=sums, first=3, recent=7, tensors=(rows_of("uint8", 4),), seed=2).evict()
 
 
+@pytest.mark.parametrize("s,h,n,budget", [(4, 8, 17001, 3000), (3, 11, 17001, 16990), (40, 8, 1100, 600), (256, 8, 1500, 1400), (64, 16, 1700, 900), (130, 8, 300, 299), (1, 33, 33000, 32990)])
+def test_routes_of_large_batches(nms, s, h, n, budget):
+    """Batches on either side of the rules: several workgroups to a frame or one, one vector of slots to a lane or two, weights with the cut or before it."""
+    for tokens in (1, 4):
+        Cache(nms, s, h, n, budget, first=3, recent=20, counts=np.random.default_rng(n).integers(0, n + 1, s), weights=attention(s, h, 4, tokens, n, "bf16", n),
+              tensors=(rows_of("uint8", 4),), seed=n).evict()
+
+
+@pytest.mark.parametrize("n", [900, 3000, 20000, 50000])
+@pytest.mark.parametrize("ties", [1, 2, 60])
+def test_one_row_goes(nms, n, ties):
+    """A step of one token: the least sum goes, of several such the highest slot."""
+    c = Cache(nms, 2, 2, n, n - 1, recent=5, tensors=(rows_of("float16", 32),), seed=n)
+    c.sums += 1.0
+    c.sums[:, :, np.random.default_rng(1).choice(n, ties, replace=False)] = 0.25
+    c.evict()
+    c.positions[:] = 0                                   # all protected: the last slot's row goes
+    c.window = (1, 0)
+    c.evict()
+
+
 @pytest.mark.parametrize("n,budget", [(700, 300), (4097, 1000), (9001, 8000), (40000, 5000)])
 def test_few_values_and_every_kind_of_sum(nms, n, budget):
     g = np.random.default_rng(n)
