@@ -375,6 +375,7 @@ enum { NMS_TYPE_F32 = 0, NMS_TYPE_F16 = 1, NMS_TYPE_BF16 = 2 };
 #define NMS_MAX_DRAFTS 1024          /* largest drafts_max accepted */
 #define NMS_MAX_VOCABULARY 4194304   /* largest vocabulary accepted */
 #define NMS_MAX_SLOTS 1048576        /* largest number of slots of a cache accepted */
+#define NMS_MAX_QUERY_ROWS 1048576   /* largest group * tokens of nms_cache_weights accepted */
 #define NMS_CACHE_MAX_TENSORS 8      /* tensors that one call moves */
 
 /*
@@ -432,15 +433,15 @@ int nms_verify_batched(const void *target, long long target_stride, const void *
  *   moves_out  int32 [sequences][heads][nms_cache_moves_max(n_max, budget) + 1][2]: the number of moves and 0, then pairs
  *              (to, from), to ascending, from ascending; entries behind them are left as they are; NULL: not wanted
  *   workspace  >= nms_cache_workspace_bytes(n_max, heads, sequences, budget) bytes, 256-byte aligned
- * n_max <= NMS_MAX_SLOTS, sequences * heads <= NMS_MAX_FRAMES, budget, first and recent >= 0.
+ * n_max <= NMS_MAX_SLOTS, sequences * heads <= NMS_MAX_FRAMES, group * tokens <= NMS_MAX_QUERY_ROWS; budget, first and recent >= 0.
  */
 typedef struct nms_cache_weights {
     const void *weights;          /* device [sequences][heads][group][tokens][columns] of `type`, row_stride elements from row to row */
     long long row_stride;         /* >= columns */
     int32_t type;                 /* NMS_TYPE_* */
-    int32_t group;                /* query heads that share a cached head, >= 1 */
-    int32_t tokens;               /* query rows per query head, >= 1 */
-    int32_t columns;              /* slots that have a weight; those at or beyond it get none */
+    int32_t group;                /* query heads that share a cached head */
+    int32_t tokens;               /* query rows per query head */
+    int32_t columns;              /* slots that have a weight; those at or beyond it get none (group, tokens or columns 0: nothing is added) */
     const int32_t *valid_tokens;  /* device [sequences]: how many of the query rows count, from the first (clamped to [0, tokens]); NULL: all */
 } nms_cache_weights;
 /* A tensor whose rows move with their slots: row (sequence, head, slot) begins at rows + sequence * sequence_stride +

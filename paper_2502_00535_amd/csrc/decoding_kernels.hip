@@ -26,6 +26,9 @@ __device__ __forceinline__ int frame_count(const int32_t *counts, int s, int n_m
     return c < 0 ? 0 : (c > n_max ? n_max : c);
 }
 
+// The wavefront's number in its workgroup, known to be the same in all lanes: branches and addresses that depend on it are scalar.
+__device__ __forceinline__ int wave_of_thread() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 #include "kernels/verify.h"
 #include "kernels/cache_move.h"
 #include "kernels/cache_keep.h"
@@ -79,6 +82,7 @@ int weights_status(const nms_cache_weights *w)
 {
     if (w == nullptr) return NMS_OK;
     if (!known_type(w->type) || w->group < 0 || w->tokens < 0 || w->columns < 0 || w->row_stride < w->columns) return NMS_ERR_INVALID_ARG;
+    if ((long long)w->group * w->tokens > NMS_MAX_QUERY_ROWS) return NMS_ERR_TOO_LARGE;
     if (w->weights == nullptr && w->group > 0 && w->tokens > 0 && w->columns > 0) return NMS_ERR_INVALID_ARG;
     return NMS_OK;
 }

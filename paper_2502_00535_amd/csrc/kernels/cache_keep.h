@@ -93,27 +93,31 @@ template <typename T>
 __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, WeightArgs w)
 {
     __shared__ double room[kAddWaves - 1][4][64];
-    const int frame = blockIdx.y, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int frame = blockIdx.y, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = wave_of_thread();
     const int n = min(slots_of(a, sequence), w.columns), i = blockIdx.x * kAddSlots + lane * 4;
     if ((int)blockIdx.x * kAddSlots >= n) return;
     const bool whole = (int)(blockIdx.x + 1) * kAddSlots <= n;
     const int tokens = valid_of(w, sequence), rows = w.group * tokens;
     const T *first = static_cast<const T *>(w.weights) + (long long)frame * w.group * w.tokens * w.row_stride;
+    const long long gap = (long long)(w.tokens - tokens) * w.row_stride;  // between the valid rows of two query heads
     double sum[4];
     constexpr int kRows = 8;
     for (bool look : {false, true}) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = 0.0;
-        for (int r0 = wave; r0 < rows; r0 += kAddWaves * kRows) {
+        const T *at = first;      // of row r; t: its token
+        int t = wave;
+        for (; t >= tokens && tokens > 0; t -= tokens) at += w.tokens * w.row_stride;
+        at += t * w.row_stride;
+        for (int r = wave; r < rows;) {
             Four<T> x[kRows];
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
-                const int r = r0 + u * kAddWaves, g = r / tokens;
                 x[u] = {};
-                if (r < rows) {
-                    const T *at = first + ((long long)g * w.tokens + (r - g * tokens)) * w.row_stride;
-                    x[u] = whole ? *reinterpret_cast<const Four<T> *>(at + i) : load_four(at, i, n);
-                }
+                if (r < rows) x[u] = whole ? *reinterpret_cast<const Four<T> *>(at + i) : load_four(at, i, n);
+                r += kAddWaves;
+                at += kAddWaves * w.row_stride;
+                for (t += kAddWaves; t >= tokens && r < rows; t -= tokens) at += gap;
             }
             if (look) {
 #pragma unroll
@@ -287,7 +291,7 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     extern __shared__ float moved_sums[];  // (with weights) moves_max of them, of
     uint16_t *targets = reinterpret_cast<uint16_t *>(moved_sums + (kWeights ? a.moves_max : 0));  // rows that move into these slots, in order,
     uint16_t *sources = targets + a.moves_max;                                                     // from these
-    const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = wave_of_thread(), waves = blockDim.x >> 6;
     const int n = slots_of(a, sequence), k = min(n, a.budget);
     const long long base = (long long)frame * a.n_max;
     const long long since = (long long)(a.lengths != nullptr ? a.lengths[sequence] : n) - a.recent;  // places at or beyond it are protected

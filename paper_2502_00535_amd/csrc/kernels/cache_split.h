@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kCutThreads) cache_split_cut_kernel(CacheArgs 
 {
     __shared__ uint32_t bins[kSplitBins], wave_sums[kCutWaves], found[3], few;
     __shared__ unsigned long long list[kSplitList];
-    const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int frame = blockIdx.x, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = wave_of_thread();
     const int n = slots_of(a, sequence), k = min(n, a.budget);
     const int parts = (k + x.part - 1) / x.part + (n - k + x.part - 1) / x.part;
     if (k == 0 || k == n) {  // none stays, or all
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kSplitThreads) cache_split_keep_kernel(CacheAr
 {
     constexpr int kWaves = kSplitThreads / 64, kRounds = 4;  // rounds of 1024 slots, 256 to a wavefront
     __shared__ uint32_t room[kWaves], ranks[2];
-    const int frame = blockIdx.y, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = blockIdx.x;
+    const int frame = blockIdx.y, sequence = frame / a.heads, lane = threadIdx.x & 63, wave = wave_of_thread(), part = blockIdx.x;
     const int n = slots_of(a, sequence), k = min(n, a.budget);
     const int low = (k + x.part - 1) / x.part, parts = low + (n - k + x.part - 1) / x.part;
     const long long base = (long long)frame * a.n_max;

@@ -274,7 +274,7 @@ constexpr int kVerifySumWaves = 4;
 template <typename T, bool kDraft>
 __global__ void __launch_bounds__(kVerifySumWaves * 64) verify_sums_kernel(VerifyArgs a, int segments, VerifyScratch to)
 {
-    const int s = blockIdx.y, lane = threadIdx.x & 63, g = blockIdx.x * kVerifySumWaves + (threadIdx.x >> 6);
+    const int s = blockIdx.y, lane = threadIdx.x & 63, g = blockIdx.x * kVerifySumWaves + wave_of_thread();
     if (g >= segments) return;
     int count;
     const int accepted = count_accepted<T, kDraft>(a, s, lane, count);
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs a, in
 {
     __shared__ double sums[kVerifyMaxSegments];
     __shared__ DrawRoom room;
-    const int s = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int s = blockIdx.x, lane = threadIdx.x & 63, wave = wave_of_thread();
     int2 found;
     if (kGiven) found = given.accepted[s];
     else found.x = count_accepted<T, kDraft>(a, s, lane, found.y);

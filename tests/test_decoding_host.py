@@ -163,6 +163,7 @@ def test_refusals_of_eviction(nms):
                nms.NmsCachePages(0x1000, 4, 16, -1, 0), nms.NmsCachePages(0x1000, 4, 16, 9, 1), nms.NmsCachePages(0x1000, -4, -16, 9, 0)):
         assert evict(pg=pg) == bad and move(pg=pg) == bad
     assert move(moves=None) == bad
+    assert evict(w=weights(group=1025, tokens=1024)) == large and keep(w=weights(group=2147483647, tokens=2147483647)) == large
     need = nms.nms_cache_workspace_bytes(50, 2, 3, 10)
     for wrong in (dict(ws=None), dict(size=need - 1), dict(ws=ctypes.c_void_p(0x1010))):
         assert evict(**wrong) == nms.NMS_ERR_WORKSPACE and keep(**wrong) == nms.NMS_ERR_WORKSPACE, wrong
