@@ -178,6 +178,25 @@ __device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) { return of_lane(wave_fold(x, [](uint32_t p, uint32_t q) { return max(p, q); }), 63); }
 __device__ __forceinline__ uint32_t wave_running_count(uint32_t x) { return wave_fold(x, [](uint32_t p, uint32_t q) { return p + q; }); }
 
+// The first bins are chosen for sums of attention weights: 32 binary orders from 2^-24 to 2^8 (with 2048 bins 64 to an order; the bin of the cut then
+// holds some 0.3 % of the rows), whatever lies outside in the first and the last but one; the last is for protected rows.  So keys can be counted while
+// others are still on their way.
+constexpr uint32_t kBinsBase = 0x80000000u + (103u << 23) + 1u;  // key of 2^-24
+constexpr int kBinsLog = 28;                                     // logarithm of how many keys the orders hold
+__device__ __forceinline__ uint32_t key_bin(uint32_t key, int shift, uint32_t last)
+{
+    const uint32_t bin = min((key < kBinsBase ? 0u : key - kBinsBase) >> shift, last - 1u);
+    return key == NMS_CACHE_KEY_PROTECTED ? last : bin;
+}
+__device__ __forceinline__ uint32_t bin_begin(uint32_t bin, int shift, uint32_t last)
+{
+    return bin == 0u ? 1u : bin == last ? NMS_CACHE_KEY_PROTECTED : kBinsBase + (bin << shift);
+}
+__device__ __forceinline__ uint32_t bin_end(uint32_t bin, int shift, uint32_t last)
+{
+    return bin == last ? NMS_CACHE_KEY_PROTECTED : bin_begin(bin + 1u, shift, last) - 1u;
+}
+
 struct KeepRoom {
     uint32_t bins[kKeepBins];
     uint32_t wave_a[kKeepMaxWaves], wave_b[kKeepMaxWaves], wave_c[kKeepMaxWaves];
@@ -185,32 +204,74 @@ struct KeepRoom {
     uint32_t few, few_keys[kFew];
 };
 
-// Where the best `need` of the `left` keys between lo and hi end (0 < need <= left; exact: lo is one of them): at the least that stays, and how many keys equal to it are
-// wanted and there.
+// Four keys of a lane into the bins: bin(key) names one of them, or kNoBin.  An atomic addition in LDS per key; where the lanes of a wavefront crowd
+// into one bin (equal sums: they would queue up there) they are added as one.
+constexpr uint32_t kNoBin = ~0u;
+template <typename Bin>
+__device__ __forceinline__ void count_four(KeepRoom &room, const uint32_t *key, Bin &&bin, int lane)
+{
+    const uint32_t first = bin(key[0]);
+    const unsigned long long in0 = __ballot(first != kNoBin);
+    const unsigned long long same0 = in0 != 0 ? __ballot(first == of_lane(first, __builtin_ctzll(in0))) : 0ull;
+    if (__popcll(same0) <= 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t b = bin(key[j]);
+            if (b != kNoBin) atomicAdd(&room.bins[b], 1u);
+        }
+    } else {
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t b = bin(j == 0 ? key[0] : j == 1 ? key[1] : j == 2 ? key[2] : key[3]);
+            const unsigned long long in = __ballot(b != kNoBin);
+            if (in == 0) continue;
+            const unsigned long long same = __ballot(b == of_lane(b, __builtin_ctzll(in))), leader = same & (0ull - same);
+            if (((in & ~same) | leader) >> lane & 1) atomicAdd(&room.bins[b], (leader >> lane & 1) != 0 ? (uint32_t)__popcll(same) : 1u);
+        }
+    }
+}
+
+// The bin in which the need-th of the counted keys lies, `left` of them in all; afterwards the need-th of the `left` in that bin is looked for.
+__device__ __forceinline__ uint32_t choose_bin(KeepRoom &room, uint32_t &need, uint32_t &left, int wave, int lane)
+{
+    __syncthreads();
+    // thread t has bins 2 t and 2 t + 1; how many keys lie in larger bins
+    const uint32_t b0 = room.bins[2 * threadIdx.x], b1 = room.bins[2 * threadIdx.x + 1], own = b0 + b1;
+    const uint32_t upto = wave_running_count(own);
+    if (lane == 63) room.wave_a[wave] = upto;
+    __syncthreads();
+    uint32_t below = 0;
+    for (int i = 0; i < wave; ++i) below += room.wave_a[i];
+    const uint32_t above = left - (below + upto);  // in the bins of threads after this one
+    if (above < need && need <= above + own) {
+        const bool upper = need <= above + b1;
+        room.found[0] = 2 * threadIdx.x + (upper ? 1 : 0);
+        room.found[1] = upper ? above : above + b1;
+        room.found[2] = upper ? b1 : b0;
+    }
+    __syncthreads();
+    need -= room.found[1];
+    left = room.found[2];
+    return room.found[0];
+}
+
+__device__ __forceinline__ void clear_bins(KeepRoom &room)
+{
+    room.bins[threadIdx.x] = 0;
+    room.bins[blockDim.x + threadIdx.x] = 0;
+    __syncthreads();
+}
+
+// Where the best `need` of the `left` keys between lo and hi end (0 < need <= left): at the least that stays, and how many keys equal to it are
+// wanted and there.  The keys are counted in bins, the bin in which the need-th lies is cut into bins again, until few keys are left (which are
+// compared one with another), or one, or all that are left are wanted.
 struct Cut {
     uint32_t key, wanted, there;
 };
-
-// Keys are counted in bins between lo and hi, the bin in which the need-th lies is cut into bins again, until few keys are left (which are compared
-// one with another), or one, or all that are left are wanted.  Counting costs an atomic addition in LDS per key and round; sums of attention weights
-// spread over dozens of binary orders, so that a round or two do.  Where the lanes of a wavefront crowd into one bin (equal sums: they would queue up
-// there) they are added as one.
 template <int kVecs>
 __device__ __forceinline__ Cut find_cut(KeepRoom &room, const uint32_t (&key)[kVecs * 4], uint32_t lo, uint32_t hi, uint32_t need, uint32_t left,
-                                        bool exact, int wave, int lane)
+                                        int log_bins, int wave, int lane)
 {
-    const int log_bins = 31 - __builtin_clz(blockDim.x * 2);
-    if (left - need == 1 && exact) {  // one goes, as in a decoding step of one token: the smallest key, if no other is the same
-        uint32_t equal = 0;
-#pragma unroll
-        for (int e = 0; e < kVecs * 4; ++e) equal += __popcll(__ballot(key[e] == lo));
-        if (lane == 0) room.wave_c[wave] = equal;
-        __syncthreads();
-        equal = 0;
-        for (int i = 0; i < (int)(blockDim.x >> 6); ++i) equal += room.wave_c[i];
-        __syncthreads();
-        return equal == 1 ? Cut{lo + 1, 0u, 0u} : Cut{lo, equal - 1, equal};
-    }
     for (;;) {
         if (left == need) return {lo, 0u, 0u};    // all that are left: whatever lies at or beyond lo
         if (lo == hi) return {lo, need, left};
@@ -235,48 +296,11 @@ __device__ __forceinline__ Cut find_cut(KeepRoom &room, const uint32_t (&key)[kV
             return {of_lane(mine, which), need - of_lane(larger, which), of_lane(equal, which)};
         }
         const int bits = 32 - __builtin_clz(range), shift = bits > log_bins ? bits - log_bins : 0;
-        room.bins[threadIdx.x] = 0;
-        room.bins[blockDim.x + threadIdx.x] = 0;
-        __syncthreads();
+        clear_bins(room);
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-            const uint32_t bin0 = (key[v * 4] - lo) >> shift;
-            const unsigned long long in0 = __ballot(key[v * 4] - lo <= range);
-            const unsigned long long same0 = in0 != 0 ? __ballot(bin0 == of_lane(bin0, __builtin_ctzll(in0))) & in0 : 0ull;
-            if (__popcll(same0) <= 8) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (key[v * 4 + j] - lo <= range) atomicAdd(&room.bins[(key[v * 4 + j] - lo) >> shift], 1u);
-            } else {
-#pragma unroll 1
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t u = (j == 0 ? key[v * 4] : j == 1 ? key[v * 4 + 1] : j == 2 ? key[v * 4 + 2] : key[v * 4 + 3]) - lo, bin = u >> shift;
-                    const unsigned long long in = __ballot(u <= range);
-                    if (in == 0) continue;
-                    const unsigned long long same = __ballot(bin == of_lane(bin, __builtin_ctzll(in))) & in, leader = same & (0ull - same);
-                    if (((in & ~same) | leader) >> lane & 1) atomicAdd(&room.bins[bin], (leader >> lane & 1) != 0 ? (uint32_t)__popcll(same) : 1u);
-                }
-            }
-        }
-        __syncthreads();
-        // thread t has bins 2 t and 2 t + 1; how many keys lie in larger bins
-        const uint32_t b0 = room.bins[2 * threadIdx.x], b1 = room.bins[2 * threadIdx.x + 1], own = b0 + b1;
-        const uint32_t upto = wave_running_count(own);
-        if (lane == 63) room.wave_a[wave] = upto;
-        __syncthreads();
-        uint32_t below = 0;
-        for (int i = 0; i < wave; ++i) below += room.wave_a[i];
-        const uint32_t above = left - (below + upto);  // in the bins of threads after this one
-        if (above < need && need <= above + own) {
-            const bool upper = need <= above + b1;
-            room.found[0] = 2 * threadIdx.x + (upper ? 1 : 0);
-            room.found[1] = upper ? above : above + b1;
-            room.found[2] = upper ? b1 : b0;
-        }
-        __syncthreads();
-        need -= room.found[1];
-        left = room.found[2];
-        lo += room.found[0] << shift;
+        for (int v = 0; v < kVecs; ++v)
+            count_four(room, key + v * 4, [&](uint32_t u) { return u - lo <= range ? (u - lo) >> shift : kNoBin; }, lane);
+        lo += choose_bin(room, need, left, wave, lane) << shift;
         const uint32_t top = lo + ((1u << shift) - 1u);
         hi = top < lo || top > hi ? hi : top;
     }
@@ -298,18 +322,20 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     const int newest = since < INT32_MIN ? INT32_MIN : (int)since;
     const int base_slot = wave * (256 * kVecs) + lane * 4;
     auto slot_of = [&](int e) { return base_slot + (e >> 2) * 256 + (e & 3); };
-    uint32_t key[kEach], largest = 0, smallest = 0, guarded = 0;  // smallest: as its complement; both without the protected rows
+    // All rows stay, or none, or all but one (a decoding step of one token: the smallest key goes); else keys are counted in bins as they come in.
+    const bool one_goes = n - k == 1 && k > 0, counted = k > 0 && n - k > 1;
+    const int log_bins = 31 - __builtin_clz(blockDim.x * 2), shift = kBinsLog - log_bins;
+    auto first_bin = [&](uint32_t u) { return u != 0u ? key_bin(u, shift, (1u << log_bins) - 1u) : kNoBin; };
+    if (counted) clear_bins(room);
+    uint32_t key[kEach];
     auto take = [&](auto whole, int v, const Four<float> &s, const Four<int32_t> &p) {  // whole: every slot of the wavefront holds a row
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const bool there = decltype(whole)::value || base_slot + v * 256 + j < n;
-            const bool protect = p.v[j] < a.first || p.v[j] >= newest;
-            const uint32_t u = there ? live_key(s.v[j], protect) : 0u, among = protect ? 0u : u;
-            key[v * 4 + j] = u;
-            largest = max(largest, among);
-            smallest = max(smallest, among != 0u ? ~u : 0u);
-            guarded += u == NMS_CACHE_KEY_PROTECTED;
+            const uint32_t u = live_key(s.v[j], p.v[j] < a.first || p.v[j] >= newest);
+            key[v * 4 + j] = there ? u : 0u;
         }
+        if (counted) count_four(room, key + v * 4, first_bin, lane);
     };
     auto places = [&](auto whole, int v) {
         const int i = base_slot + v * 256;
@@ -402,23 +428,35 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
 #pragma unroll
         for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] != 0u) << e;
     } else if (k > 0) {
-        largest = wave_max(largest);
-        smallest = wave_max(smallest);
-        guarded = wave_running_count(guarded);
-        if (lane == 63) room.wave_a[wave] = largest, room.wave_b[wave] = smallest, room.wave_c[wave] = guarded;
-        __syncthreads();
-        guarded = 0;
-        for (int i = 0; i < waves; ++i) {
-            largest = max(largest, room.wave_a[i]);
-            smallest = max(smallest, room.wave_b[i]);
-            guarded += room.wave_c[i];
+        uint32_t lo = 0, hi = 0, need = (uint32_t)k, left = (uint32_t)n;
+        if (one_goes) {
+            uint32_t least = ~0u;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) least = min(least, key[e] - 1u);  // of 0, where there is no row: the largest number
+            least = wave_max(~least);
+            if (lane == 63) room.wave_a[wave] = least;
+            __syncthreads();
+            for (int i = 0; i < waves; ++i) least = max(least, room.wave_a[i]);
+            least = ~least + 1u;
+            uint32_t equal = 0;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) equal += __popcll(__ballot(key[e] == least));
+            if (lane == 0) room.wave_b[wave] = equal;
+            __syncthreads();
+            equal = 0;
+            for (int i = 0; i < waves; ++i) equal += room.wave_b[i];
+            lo = hi = equal == 1 ? least + 1u : least;  // no other is the same: whatever lies beyond it stays
+            need = equal == 1 ? (uint32_t)k : equal - 1u;
+            left = equal == 1 ? (uint32_t)k : equal;
+            __syncthreads();
+        } else {
+            const uint32_t bin = choose_bin(room, need, left, wave, lane), last = (1u << log_bins) - 1u;
+            lo = bin_begin(bin, shift, last);
+            hi = bin_end(bin, shift, last);
         }
-        __syncthreads();
-        uint32_t lo = ~smallest, hi = largest, need = (uint32_t)k - guarded, left = (uint32_t)n - guarded;
-        if ((uint32_t)k <= guarded) lo = hi = NMS_CACHE_KEY_PROTECTED, need = (uint32_t)k, left = guarded;  // protected rows alone
         Cut cut;
-        for (bool exact = true;; exact = false) {
-            cut = find_cut<kVecs>(room, key, lo, hi, need, left, exact, wave, lane);
+        for (;;) {
+            cut = find_cut<kVecs>(room, key, lo, hi, need, left, log_bins, wave, lane);
             const bool ties = cut.wanted < cut.there;
 #pragma unroll
             for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] > cut.key || (key[e] == cut.key && !ties)) << e;

@@ -7,19 +7,10 @@
 // frame, from the parts' counts and then from the keys of one bin; the third, by parts again, writes keep bytes and moves.  A part lies wholly below
 // slot k or wholly at or beyond it, so that its free slots and its moving rows follow from how many of its rows stay.
 //
-// The bins are chosen for sums of attention weights: 64 to a binary order from 2^-24 to 2^8, whatever lies outside in the first and the last.
-// (The bin of the cut then holds some 250 of 100,000 rows.)  A bin that holds more rows than LDS takes is counted again, finer, from memory.
-constexpr int kSplitBins = 2048;
-constexpr uint32_t kSplitBase = 0x80000000u + (103u << 23) + 1u;  // key of 2^-24
-constexpr int kSplitShift = 17;
+// A bin that holds more rows than LDS takes is counted again, finer, from memory.
+constexpr int kSplitBins = 2048, kSplitShift = kBinsLog - 11;
 constexpr int kSplitThreads = 256;
 constexpr int kSplitList = 4096;
-
-__device__ __forceinline__ uint32_t split_bin(uint32_t key)
-{
-    const uint32_t v = key < kSplitBase ? 0u : (key - kSplitBase) >> kSplitShift;
-    return min(v, (uint32_t)(kSplitBins - 1));
-}
 
 struct SplitArgs {
     uint32_t *keys;             // [frames][n_max]
@@ -60,7 +51,7 @@ __global__ void __launch_bounds__(kSplitThreads) cache_split_keys_kernel(CacheAr
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u.v[j] = live_key(s.v[j], p.v[j] < a.first || p.v[j] >= newest);
-            bin[j] = split_bin(u.v[j]);
+            bin[j] = key_bin(u.v[j], kSplitShift, kSplitBins - 1);
         }
         store_four(x.keys + base, i, range.y, u);
         const unsigned long long in = __ballot(i < range.y);
@@ -139,9 +130,8 @@ __global__ void __launch_bounds__(kCutThreads) cache_split_cut_kernel(CacheArgs 
     };
     {
         const uint32_t bin = choose();
-        lo = bin == 0 ? 0ull : (unsigned long long)(kSplitBase + (bin << kSplitShift)) << 32;
-        hi = bin == kSplitBins - 1 ? ~0ull : (unsigned long long)(kSplitBase + ((bin + 1) << kSplitShift)) << 32;
-        if (bin != kSplitBins - 1) --hi;
+        lo = (unsigned long long)bin_begin(bin, kSplitShift, kSplitBins - 1) << 32;
+        hi = (unsigned long long)bin_end(bin, kSplitShift, kSplitBins - 1) << 32 | 0xffffffffull;
     }
     const uint32_t first_bin = found[0];
     bool listed = false, recounted = false;  // the rows between lo and hi are in LDS; they were counted again from memory

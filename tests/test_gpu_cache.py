@@ -158,6 +158,19 @@ def test_routes_of_large_batches(nms, s, h, n, budget):
               tensors=(rows_of("uint8", 4),), seed=n).evict()
 
 
+@pytest.mark.parametrize("n,budget", [(900, 500), (5000, 4900), (30000, 8000), (50000, 3)])
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1.0, 300.0, 1e6, 1e35])
+def test_sums_of_every_size(nms, n, budget, scale):
+    """Sums far from those that the counting expects, alone and next to such, below zero and beside protected rows and infinite ones."""
+    c = Cache(nms, 2, 2, n, budget, 1, budget // 3, tensors=(rows_of("uint8", 4),), seed=n)
+    c.sums[0] *= np.float32(scale)
+    c.sums[1, :, ::2] *= np.float32(-scale)
+    c.sums[1, :, ::7] = np.inf
+    c.evict()
+    c.window = (0, 0)
+    c.steps()
+
+
 @pytest.mark.parametrize("n", [900, 3000, 20000, 50000])
 @pytest.mark.parametrize("ties", [1, 2, 60])
 def test_one_row_goes(nms, n, ties):
