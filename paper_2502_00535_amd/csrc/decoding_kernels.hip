@@ -187,19 +187,19 @@ int keep_and_move(const CacheArgs &a, const nms_cache_weights *weights, const Mo
 {
     WeightArgs w = weight_args(weights);
     const int type = weights != nullptr ? weights->type : 0;
-    if (w.weights != nullptr && !nms_cache_add_with_keep(a.n_max, frames, w.group * (long long)w.tokens)) {
+    const bool few = a.moves_max <= NMS_CACHE_FEW, many = !few && (a.moves != nullptr || a.move_sums);
+    if (w.weights != nullptr && !nms_cache_add_with_keep(a.n_max, frames, many, w.group * (long long)w.tokens)) {
         const int st = add_launch(a, w, type, frames, stream);
         if (st != NMS_OK) return st;
         w = {};
     }
-    if (nms_cache_split(a.n_max, frames)) {
+    if (nms_cache_split(a.n_max, frames, many)) {
         const int st = split_launch(a, scratch, frames, stream);
         if (st != NMS_OK) return st;
         MoveArgs with_sums = m;
         if (a.move_sums) with_sums.sums = a.sums, with_sums.positions = a.positions;
         return move_launch(with_sums, frames, stream);
     }
-    const bool few = a.moves_max <= kFew;
     CacheArgs b = a;
     if (few && a.move_sums) b.moves = nullptr;  // the list stays in LDS
     const MoveArgs none = {}, &now = few ? m : none;

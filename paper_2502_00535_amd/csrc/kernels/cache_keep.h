@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, 
 // count over the wavefronts before, the vectors before, the lanes before and the lane's own.
 constexpr int kKeepMaxWaves = NMS_CACHE_WAVES;
 constexpr int kKeepBins = kKeepMaxWaves * 64 * 2;  // two to a thread
-constexpr int kFew = 64;                           // candidates that are compared one with another; moves that need no list in memory
+constexpr int kFew = 64;                           // candidates that are compared one with another
 
 // Keys of slots that hold a row are at least 1, so that 0 can stand for those that hold none.
 __device__ __forceinline__ uint32_t live_key(float sum, bool protect)

@@ -36,10 +36,12 @@ NMS_HD int nms_moves_max(int n_max, int budget)
 static inline size_t nms_decoding_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // ---- eviction: the route ------------------------------------------------------------------------
 // A frame is one workgroup with the keys of all its slots in registers, or (split) is shared by several workgroups in three launches: frames that
-// registers do not hold, and long ones of small batches.  Keep vector alone, us, one workgroup / split: 8 x 16,384 slots 11.6 / 16.0; 8 x 32,768
-// 17.8 / 17.9; 64 x 32,768 20.3 / 24.2; 512 x 32,768 50 / 76.  Whole path with 64 query rows: 8 x 16,384 35.6 / 35.6; 32 x 32,768 91 / 82.
+// registers do not hold, and long ones of small batches where many rows move.  Keep vector alone, us, one workgroup / split: 8 x 16,384 slots 11.7 / 15.9;
+// 8 x 32,768 17.1 / 17.3; 32 x 32,768 17.3 / 21.9; 64 x 32,768 17.9 / 24.3.  Whole path with 64 query rows: 8 x 20,000 50.6 / 41.5; 16 x 32,768 59.5 / 53.0;
+// 32 x 32,768 86.2 / 84.1; 64 x 32,768 151 / 154; 32 x 16,384 49.2 / 57.5.
 #define NMS_CACHE_WAVES 16   // most wavefronts to a workgroup
-static inline bool nms_cache_split(int n_max, int frames) { return n_max > 32768 || (n_max > 16384 && frames <= 32); }
+#define NMS_CACHE_FEW 64     // moves that need no list in memory: their rows move in the same launch
+static inline bool nms_cache_split(int n_max, int frames, bool many_moves) { return n_max > 32768 || (n_max > 16384 && frames <= 32 && many_moves); }
 // Vectors of four slots to a lane: one while sixteen wavefronts reach and the batch's wavefronts are on the chip at once, two or more otherwise.  A step
 // of one token, us, one vector / two (bf16 weights): 8 heads x 2001 slots 9.1 / 10.7; 8 x 3501 10.3 / 10.6; 512 x 2001 11.6 / 12.5; 1024 x 1501
 // (6144 wavefronts) 13.2 / 13.7; 512 x 3501 (7168) 20.0 / 14.5; 1024 x 2501 28.1 / 18.2; 2048 x 1501 27.3 / 20.0.
@@ -53,9 +55,9 @@ static inline int nms_cache_vecs(int n_max, int frames)
 // The weights are added by the launch that finds the rows that stay where there are few query rows, by one of its own otherwise.  Whole call, us, with it /
 // on their own (bf16): 4 query rows, 8 x 4001 11.5 / 12.6, 512 x 2001 12.2 / 20.3; 16, 8 x 4001 16.9 / 13.2, 256 x 4001 23.4 / 23.9, 1024 x 1001 18.5 / 23.5;
 // 32, 8 x 4001 24.1 / 14.1, 256 x 4001 36.8 / 30.6, 1024 x 1001 27.8 / 29.7.
-static inline bool nms_cache_add_with_keep(int n_max, int frames, long long rows)
+static inline bool nms_cache_add_with_keep(int n_max, int frames, bool many_moves, long long rows)
 {
-    return !nms_cache_split(n_max, frames) && nms_cache_vecs(n_max, frames) <= 4 && (rows <= 8 || (rows <= 16 && frames >= 1024));
+    return !nms_cache_split(n_max, frames, many_moves) && nms_cache_vecs(n_max, frames) <= 4 && (rows <= 8 || (rows <= 16 && frames >= 1024));
 }
 
 // Scratch: the list of moves (of the whole path), and what the three launches hand on.
@@ -70,8 +72,10 @@ struct NmsSplitLayout {
 static inline NmsSplitLayout nms_split_layout(int n_max, int frames)
 {
     NmsSplitLayout l;
-    l.part = 4096;  // the largest part that still makes two workgroups to a compute unit
-    while (l.part > 1024 && (long long)frames * (n_max / l.part) < 512) l.part /= 2;
+    // The largest part, or a smaller one where that leaves compute units idle and the cut's workgroup does not have the counts of more than 64 parts to add
+    // up.  Keep vector alone, us, 1024 / 2048 / 4096 slots: 1 x 100,003 27.9 / 24.2 / -; 8 x 100,003 33.2 / - / 27.3; 8 x 20,000 18.2 / 21.0 / -.
+    l.part = 4096;
+    while (l.part > 1024 && (long long)frames * (n_max / l.part) < 128 && n_max / (l.part / 2) <= 64) l.part /= 2;
     l.parts = (n_max + l.part - 1) / l.part + 1;
     l.keys = 0;
     l.bins = l.keys + nms_decoding_align256((size_t)frames * n_max * sizeof(uint32_t));
@@ -82,7 +86,7 @@ static inline NmsSplitLayout nms_split_layout(int n_max, int frames)
 }
 static inline size_t nms_cache_scratch(int n_max, int frames, int budget)
 {
-    return nms_cache_list_bytes(n_max, frames, budget) + (nms_cache_split(n_max, frames) ? nms_split_layout(n_max, frames).bytes : 0);
+    return nms_cache_list_bytes(n_max, frames, budget) + (nms_cache_split(n_max, frames, true) ? nms_split_layout(n_max, frames).bytes : 0);
 }
 
 // ---- verification: the cut of a row, and the route -------------------------------------------

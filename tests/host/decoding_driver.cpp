@@ -24,11 +24,11 @@ int main(int argc, char **argv)
         while (std::scanf("%d %d", &n, &b) == 2) std::printf("%d %zu\n", nms_moves_max(n, b), nms_cache_scratch(n, 3, b));
         return 0;
     }
-    if (!std::strcmp(argv[1], "route")) {         // n_max frames rows -> split, vectors, with weights, part, parts, bytes, offsets of the split's scratch
-        int n, f, rows;
-        while (std::scanf("%d %d %d", &n, &f, &rows) == 3) {
+    if (!std::strcmp(argv[1], "route")) {         // n_max frames rows many -> split, vectors, with weights, part, parts, bytes, offsets of the split's scratch
+        int n, f, rows, many;
+        while (std::scanf("%d %d %d %d", &n, &f, &rows, &many) == 4) {
             const NmsSplitLayout l = nms_split_layout(n, f);
-            std::printf("%d %d %d %d %d %zu %zu %zu %zu %zu\n", nms_cache_split(n, f), nms_cache_vecs(n, f), nms_cache_add_with_keep(n, f, rows), l.part, l.parts, l.keys,
+            std::printf("%d %d %d %d %d %zu %zu %zu %zu %zu\n", nms_cache_split(n, f, many), nms_cache_vecs(n, f), nms_cache_add_with_keep(n, f, many, rows), l.part, l.parts, l.keys,
                         l.bins, l.cuts, l.stays, l.bytes);
         }
         return 0;

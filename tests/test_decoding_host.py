@@ -66,8 +66,8 @@ def test_routes_of_eviction_fit_their_kernels(driver):
     """One workgroup: at most sixteen wavefronts whose lanes hold every slot, 16-bit slot numbers, the lists within 160 KiB of LDS.  Several: parts that
     cover the frame with one to spare, 16-bit counts, a list of parts within the cut's LDS, and scratch without overlaps."""
     sizes = sorted({1, 2, 255, 256, 1023, 1024, 1025, 2048, 3583, 3584, 3585, 4096, 4097, 8192, 8193, 16384, 16385, 32768, 32769, 65536, 100003, 524288, 1048575, 1048576})
-    cases = [(n, f, r) for n in sizes for f in (1, 8, 32, 33, 300, 512, 1024, 65535) for r in (1, 8, 9, 16, 17)]
-    for (n, f, rows), line in zip(cases, driver("route", [" ".join(map(str, c)) for c in cases])):
+    cases = [(n, f, r, m) for n in sizes for f in (1, 8, 32, 33, 300, 512, 1024, 65535) for r in (1, 8, 9, 16, 17) for m in (0, 1)]
+    for (n, f, rows, many), line in zip(cases, driver("route", [" ".join(map(str, c)) for c in cases])):
         split, vecs, together, part, parts, keys, bins, cuts, stays, total = (int(x) for x in line.split())
         if not split:
             waves = -(-n // (256 * vecs))

@@ -150,7 +150,7 @@ def test_ties_everywhere(nms, s, h, n, budget, sums):
     Cache(nms, s, h, n, budget, sums=sums, first=3, recent=7, tensors=(rows_of("uint8", 4),), seed=2).evict()
 
 
-@pytest.mark.parametrize("s,h,n,budget", [(4, 8, 17001, 3000), (3, 11, 17001, 16990), (40, 8, 1100, 600), (256, 8, 1500, 1400), (64, 16, 1700, 900), (130, 8, 300, 299), (1, 33, 33000, 32990)])
+@pytest.mark.parametrize("s,h,n,budget", [(4, 8, 17001, 3000), (3, 11, 17001, 16990), (40, 8, 1100, 600), (256, 8, 1500, 1400), (64, 16, 1700, 900), (130, 8, 300, 299), (1, 33, 33000, 32990), (5, 8, 20000, 3000), (1, 33, 32768, 16384)])
 def test_routes_of_large_batches(nms, s, h, n, budget):
     """Batches on either side of the rules: several workgroups to a frame or one, one vector of slots to a lane or two, weights with the cut or before it."""
     for tokens in (1, 4):
