@@ -27,6 +27,10 @@ __device__ __forceinline__ int count_accepted(const VerifyArgs &a, int s, int la
     const T *target = static_cast<const T *>(a.target) + (long long)s * (a.drafts_max + 1) * a.target_stride;
     const T *draft = kDraft ? static_cast<const T *>(a.draft) + (long long)s * a.drafts_max * a.draft_stride : nullptr;
     count = a.counts != nullptr ? a.counts[s] : a.drafts_max;
+    if (a.drafts_max == 0) {
+        count = min(count, 0);
+        return 0;
+    }
     for (int i0 = 0; i0 < a.drafts_max; i0 += 64) {
         const int i = i0 + lane;
         int x = -1;

@@ -79,6 +79,14 @@ def test_counts_of_a_padded_batch(nms, with_draft):
     assert accepted[2] == 0 and (tokens[2] == -1).all() and (tokens[6] == -1).all() and tokens[1, 0] >= 0
 
 
+@pytest.mark.parametrize("v", [700, 60001])
+def test_counts_where_there_is_no_room_for_drafts(nms, v):
+    """A plain draw: counts above 0 are 0, below 0 there is no sequence."""
+    target, _, drafts, u = inputs(4, 0, v, "f32", False, 9)
+    tokens, accepted = agree(nms, target, None, drafts, [5, 0, -1, 2147483647], u)
+    assert not accepted.any() and tokens[2, 0] == -1 and (tokens[[0, 1, 3], 0] >= 0).all()
+
+
 def test_a_token_does_not_depend_on_the_batch(nms):
     target, draft, drafts, u = inputs(260, 2, 9001, "bf16", True, 5)
     tokens, accepted = call(nms, target, draft, drafts, None, u)
