@@ -397,7 +397,7 @@ enum { NMS_TYPE_F32 = 0, NMS_TYPE_F16 = 1, NMS_TYPE_BF16 = 2 };
  *            sequence at this place of the batch: nothing of it is read, accepted_out 0, tokens -1
  *   uniforms [sequences][drafts_max + 1] float: drafts_max for the tests, the last for the token
  *   tokens_out [sequences][drafts_max + 1] int32, accepted_out [sequences] int32
- *   workspace  >= nms_verify_workspace_bytes(vocabulary, sequences) bytes, 256-byte aligned
+ *   workspace  >= nms_verify_workspace_bytes(vocabulary, sequences) bytes, 256-byte aligned; may be NULL when that is 0
  * sequences == 0 is NMS_OK; vocabulary must be at least 1, strides at least vocabulary.
  */
 size_t nms_verify_workspace_bytes(int vocabulary, int sequences);   /* host-only, pure; 0 on invalid arguments */
@@ -446,7 +446,8 @@ typedef struct nms_cache_weights {
 } nms_cache_weights;
 /* A tensor whose rows move with their slots: row (sequence, head, slot) begins at rows + sequence * sequence_stride +
  * head * head_stride + slot * slot_stride, all in bytes, in any order of size; rows must not overlap.  With pages it begins at rows +
- * page * sequence_stride + head * head_stride + (slot % page_slots) * slot_stride, page = table[sequence * table_stride + slot / page_slots]. */
+ * page * sequence_stride + head * head_stride + (slot % page_slots) * slot_stride, page = table[sequence * table_stride + slot / page_slots].  A page belongs to one
+ * sequence: rows of pages that stand twice in the table, or in two sequences' tables, are not moved in any order. */
 typedef struct nms_cache_tensor {
     void *rows;                /* device */
     long long row_bytes;       /* 1 .. 2^20 */

@@ -6,7 +6,8 @@ The computation lives in ``libnms_mi355x.so`` (HIP, gfx950) behind the C ABI of
 calls through a small C module where that is built) with
 the same entry-point names that marshals torch tensors (device memory) and the
 current HIP stream.  There is no CPU fallback: touching any entry point without the
-built library raises ImportError.  ``python -m paper_2502_00535_amd.build`` compiles it.
+built library raises ImportError.  The same library holds the choices of a decoding step
+(verification of drafted tokens, eviction from a cache).  ``python -m paper_2502_00535_amd.build`` compiles it.
 """
 import importlib
 

@@ -7,7 +7,10 @@
 // frame, from the parts' counts and then from the keys of one bin; the third, by parts again, writes keep bytes and moves.  A part lies wholly below
 // slot k or wholly at or beyond it, so that its free slots and its moving rows follow from how many of its rows stay.
 //
-// A bin that holds more rows than LDS takes is counted again, finer, from memory.
+// The bin of the cut holds some 0.3 % of the rows; one that holds more than LDS takes is counted again, finer, from memory.
+//
+// 8 heads x 100,003 slots, us: keys 7.7, cut 13.4 (a compute unit adds up 25 parts' counts, 100 KB, and looks at 400 KB of keys), keep bytes and moves 7.2.
+// Finding the bin and listing its rows by parts, in a launch before the cut, took 18.0 + 8.1 us against 21.1 (parts of 1024 slots, 400 KB of counts).
 constexpr int kSplitBins = 2048, kSplitShift = kBinsLog - 11;
 constexpr int kSplitThreads = 256;
 constexpr int kSplitList = 4096;

@@ -3,6 +3,18 @@
 
 // ----------------------------------------------------------------------------- verification
 
+// A sequence's drafted tokens stand up to the first that the test u q < p refuses; the next token is drawn from what the target's row has beyond the
+// draft's, or from the target's row where none was refused: the least entry whose running sum passes u times the total.  So of all probabilities two
+// per drafted token and one row (or two) per sequence are read, once: the row's sum needs every entry, the entry itself one segment of it again.
+//
+// Numbers are compared and added in 64 bits: products of two floats are exact there, and with V entries in 32 bits the sum would be off by
+// up to V 2^-24 of itself, past the borders of most entries.  Conversions and additions in 64 bits take 4.5 and 5.2 cycles to a wavefront, 47 per entry
+// with both rows: less than the rows' bytes take on the whole chip (256 x 151,111 floats: 11.6 us of issue, 41 us), more than they take where a
+// compute unit has a row alone.
+//
+// Bound by: the rows' bytes for large batches (232 MB in 41 us of kernel time, 5.7 TB/s, part of it out of the last-level cache; 46.5 to 48.9 us a call);
+// for small ones by the chain of dependent loads: token, its probabilities, row, entry (1 x 32,000 floats 9.0 us, 64 x 50,001 f16 4.9 + 4.8 us in two launches).
+
 template <typename T>
 __device__ __forceinline__ float as_probability(T v)
 {
