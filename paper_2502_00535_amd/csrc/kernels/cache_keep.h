@@ -54,7 +54,8 @@ template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
 
 // Elements at or beyond `end` come out as 0.  The last vector is loaded from four elements before the end and shifted, so that a wavefront at the row's
-// end has no branch to wait in (element by element such wavefronts took 26 us where the others took 10, at 8 x 4001 slots with 32 query rows).
+// end has no branch to wait in.  Whole call, us, shifted / element by element: bf16, 8 heads x 4001 slots with 4 query rows 10.1 / 11.9, 512 x 2001 with 32
+// 29.0 / 38.2 (f32 34.8 / 50.7), the prompt of 8 x 100,003 with 128 97.8 / 126; the keep vector of 512 x 1999 8.8 / 8.6 and of 512 x 30,001 50.3 / 45.8.
 template <typename T>
 __device__ __forceinline__ Four<T> load_four(const T *row, int i, int end)
 {
@@ -94,8 +95,8 @@ __device__ __forceinline__ void store_four(T *row, int i, int end, const Four<T>
 
 // sums[i] += the weights of slot i, by a launch of its own where there are many query rows: a wavefront has 256 neighbouring slots, the four
 // wavefronts of a workgroup share out the rows, and their sums in 64 bits meet in LDS in the same order always.  Bound by the weights'
-// bytes: eight rows are in flight to a lane (8 heads x 100,003 slots x 128 rows of bf16 58 us, 3.5 TB/s; eight slots to a lane, for 16-byte loads,
-// and four rows in flight took 58 to 64 us, sixteen rows in flight 58).
+// bytes: eight rows are in flight to a lane (8 heads x 100,003 slots x 128 rows of bf16 47 us, 4.5 TB/s).  Before rows were walked without divisions it
+// took 54 to 58, and eight slots to a lane, for 16-byte loads, 64.
 constexpr int kAddWaves = 4, kAddSlots = 256;
 template <typename T>
 __global__ void __launch_bounds__(kAddWaves * 64) cache_add_kernel(CacheArgs a, WeightArgs w)

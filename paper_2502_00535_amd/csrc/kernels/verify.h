@@ -12,7 +12,7 @@
 // with both rows: less than the rows' bytes take on the whole chip (256 x 151,111 floats: 11.6 us of issue, 41 us), more than they take where a
 // compute unit has a row alone.
 //
-// Bound by: the rows' bytes for large batches (232 MB in 41 us of kernel time, 5.7 TB/s, part of it out of the last-level cache; 46.5 to 48.9 us a call);
+// Bound by: the rows' bytes for large batches (232 MB in 41 us of kernel time under the profiler, 47.8 to 49.1 us a call: 4.8 TB/s);
 // for small ones by the chain of dependent loads: token, its probabilities, row, entry (1 x 32,000 floats 9.0 us, 64 x 50,001 f16 4.9 + 4.8 us in two launches).
 
 template <typename T>
