@@ -1,10 +1,8 @@
 // The choices of a decoding step (gfx950, wave64): how many drafted tokens stand, and which rows of a cache stay.
 //
 // As for boxes, candidates have scores, the order is total (higher score, then lower index), and the outcome says which of
-// them stand.  The kernels live in kernels/verify.h, kernels/cache_keep.h and kernels/cache_move.h (included below inside the
+// them stand.  The kernels live in kernels/verify.h, cache_move.h, cache_keep.h and cache_split.h (included below inside the
 // anonymous namespace); the launch logic and the extern "C" entry points follow.
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

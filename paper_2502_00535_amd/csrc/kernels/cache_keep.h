@@ -54,8 +54,9 @@ template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
 
 // Elements at or beyond `end` come out as 0.  The last vector is loaded from four elements before the end and shifted, so that a wavefront at the row's
-// end has no branch to wait in.  Whole call, us, shifted / element by element: bf16, 8 heads x 4001 slots with 4 query rows 10.1 / 11.9, 512 x 2001 with 32
-// 29.0 / 38.2 (f32 34.8 / 50.7), the prompt of 8 x 100,003 with 128 97.8 / 126; the keep vector of 512 x 1999 8.8 / 8.6 and of 512 x 30,001 50.3 / 45.8.
+// end has no branch to wait in: for loads that follow each other in a loop, as weights and the parts of long frames do.  Whole call, us, shifted /
+// element by element: bf16, 8 heads x 4001 slots with 4 query rows 10.1 / 11.9, 512 x 2001 with 32 29.0 / 38.2 (f32 34.8 / 50.7), the prompt of
+// 8 x 100,003 with 128 97.8 / 126.
 template <typename T>
 __device__ __forceinline__ Four<T> load_four(const T *row, int i, int end)
 {
@@ -79,6 +80,18 @@ __device__ __forceinline__ Four<T> load_four(const T *row, int i, int end)
         r.v[2] = d == 0 ? r.v[2] : d == 1 ? r.v[3] : T{};
         r.v[3] = d == 0 ? r.v[3] : T{};
     }
+    return r;
+}
+// The same, element by element: for loads that a wavefront makes once, all of them before the first is needed.  Keep vector alone, us, shifted / so:
+// 512 x 1999 slots 8.7 / 8.6, 512 x 9001 17.8 / 16.3, 256 x 30,001 26.2 / 22.3, 512 x 32,765 52.7 / 44.5.
+template <typename T>
+__device__ __forceinline__ Four<T> load_four_once(const T *row, int i, int end)
+{
+    if (i + 4 <= end) return *reinterpret_cast<const Four<T> *>(row + i);
+    Four<T> r = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < end) r.v[j] = row[i + j];
     return r;
 }
 template <typename T>
@@ -349,11 +362,13 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     auto places = [&](auto whole, int v) {
         const int i = base_slot + v * 256;
         if (a.positions == nullptr) return Four<int32_t>{{i, i + 1, i + 2, i + 3}};
-        return decltype(whole)::value ? *reinterpret_cast<const Four<int32_t> *>(a.positions + base + i) : load_four(a.positions + base, i, n);
+        if (decltype(whole)::value) return *reinterpret_cast<const Four<int32_t> *>(a.positions + base + i);
+        return kWeights ? load_four(a.positions + base, i, n) : load_four_once(a.positions + base, i, n);
     };
     auto sums_of = [&](auto whole, int v) {
         const int i = base_slot + v * 256;
-        return decltype(whole)::value ? *reinterpret_cast<const Four<float> *>(a.sums + base + i) : load_four(a.sums + base, i, n);
+        if (decltype(whole)::value) return *reinterpret_cast<const Four<float> *>(a.sums + base + i);
+        return kWeights ? load_four(a.sums + base, i, n) : load_four_once(a.sums + base, i, n);
     };
     float sum[kWeights ? kEach : 1];  // with weights: the new sums, in memory only once their places are known
     if constexpr (kWeights) {
