@@ -8,8 +8,8 @@
 // that follows (keep bytes, free slots, moving rows) is a compare with the cut and a count of lanes before one's own.
 //
 // Bound by: for long frames the bytes of sums and positions, then instructions (1500 per wavefront at 8 vectors to a lane); for short ones the chain of loads, barriers
-// (five) and stores.  Kernel time, us: 8 heads x 1025 slots with four query rows and the move of one row 8.4, 512 x 2049 11.3; the keep vector of
-// 512 x 1999 7.3 (8 MB), 512 x 32,768 44 (151 MB, 3.4 TB/s; a compute unit loads a frame, then works on it); 32 x 16,384 with 1800 moves each 18.9.
+// (five) and stores.  Kernel time, us: 8 heads x 1025 slots with four query rows and the move of one row 8.2, 512 x 2049 11.3; the keep vector of
+// 512 x 1999 7.0 (8 MB), 512 x 32,768 44 (151 MB, 3.4 TB/s; a compute unit loads a frame, then works on it); 32 x 16,384 with 1800 moves each 18.7.
 
 struct CacheArgs {
     float *sums;

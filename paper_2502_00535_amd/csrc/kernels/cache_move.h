@@ -4,8 +4,8 @@
 // ----------------------------------------------------------------------------- moves
 
 // Rows that stay move into the slots of rows that go, and only those: the fewest bytes that leave the rows together in front, and no row is read that
-// another one overwrites.  Bound by the rows' bytes, read and written: 32 heads x 1792 rows of 256 bytes in two tensors (59 MB) 13.2 us, 4.5 TB/s;
-// 96 x some 880 of 160 bytes (54 MB) 13.8.  A lane moves up to 16 bytes, whatever divides the tensor's addresses; 32 rows to a workgroup, as many workgroups
+// another one overwrites.  Bound by the rows' bytes, read and written: 32 heads x 1792 rows of 256 bytes in two tensors (59 MB) 12.9 us, 4.6 TB/s;
+// 96 x some 880 of 160 bytes (56 MB) 13.9.  A lane moves up to 16 bytes, whatever divides the tensor's addresses; 32 rows to a workgroup, as many workgroups
 // as the sizes allow moves (those beyond a frame's own number end at once).
 
 struct MoveTensor {

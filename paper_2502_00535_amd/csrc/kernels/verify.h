@@ -12,8 +12,8 @@
 // with both rows: less than the rows' bytes take on the whole chip (256 x 151,111 floats: 11.6 us of issue, 41 us), more than they take where a
 // compute unit has a row alone.
 //
-// Bound by: the rows' bytes for large batches (232 MB in 41 us of kernel time under the profiler, 47.8 to 49.1 us a call: 4.8 TB/s);
-// for small ones by the chain of dependent loads: token, its probabilities, row, entry (1 x 32,000 floats 9.0 us, 64 x 50,001 f16 4.9 + 4.8 us in two launches).
+// Bound by: the rows' bytes for large batches (232 MB in 41 us of kernel time under the profiler, 47.5 to 49.1 us a call: 4.7 to 4.9 TB/s);
+// for small ones by the chain of dependent loads: token, its probabilities, row, entry (1 x 32,000 floats 9.0 us, 64 x 50,001 f16 4.9 + 5.0 us in two launches).
 
 template <typename T>
 __device__ __forceinline__ float as_probability(T v)
