@@ -703,7 +703,6 @@ def _cache_tensor(t, what, n_max, heads, sequences, paged):
 
 def _cache_tensors(tensors, n_max, heads, sequences, page_table):
     """Array of struct nms_cache_tensor, its length, and struct nms_cache_pages or None."""
-    tensors = list(tensors or ())
     if not tensors:
         return None, 0, None
     structs = (NmsCacheTensor * len(tensors))(*[_cache_tensor(t, f"tensors[{i}]", n_max, heads, sequences, page_table is not None)
@@ -744,7 +743,8 @@ def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page
     """tensors: up to eight of shape [sequences, heads, n_max, row ...] (any strides whose rows are whole), or with a page table
     ([sequences, pages of a sequence] int32) [pages, heads, slots of a page, row ...]."""
     n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
-    _here("moves", moves, "page_table", page_table, *(x for t in tensors or () for x in ("tensors", t)))
+    tensors = tuple(tensors or ())  # gone over more than once
+    _here("moves", moves, "page_table", page_table, *(x for t in tensors for x in ("tensors", t)))
     all_, s_ = _cache_elements(n, h, s)
     structs, many, pages = _cache_tensors(tensors, n, h, s, page_table)
     _check(lib.nms_cache_move_batched(_ptr(moves, "int32", "moves", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ else 0),
@@ -754,9 +754,10 @@ def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page
 def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
                      workspace, weights, valid_tokens, page_table):
     n, h, s = int(n_max), int(heads), int(sequences)
+    tensors = tuple(tensors or ())  # gone over more than once
     _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
           "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens, "page_table", page_table,
-          *(x for t in tensors or () for x in ("tensors", t)))
+          *(x for t in tensors for x in ("tensors", t)))
     all_, s_ = _cache_elements(n, h, s)
     w, wb = _ws(workspace)
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None

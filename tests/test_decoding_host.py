@@ -289,6 +289,24 @@ def test_binding_of_eviction(nms, recorded):
     assert len(recorded) == 4
 
 
+def test_tensors_may_come_from_an_iterator(nms, recorded, monkeypatch):
+    n, h, s, budget = 40, 2, 3, 16
+    rows = [gpu(s, h, n, 8), gpu(s, h, n, 4)]
+    moves = gpu(s * h * (nms.nms_cache_moves_max(n, budget) + 1) * 2, dtype=torch.int32)
+    rest = (gpu(s, h, n), None, None, None, n, h, s, budget, 0, 0)
+    after = (None, None, gpu(1 << 16, dtype=torch.uint8))
+    nms.nms_cache_evict_batched(*rest, iter(rows), *after)
+    nms.nms_cache_move_batched(moves, n, h, s, budget, (t for t in rows))
+    nms.CachePlan(*rest, iter(rows), *after)()
+    nms.nms_cache_evict_batched(*rest, None, *after)
+    evict, move, plan, none = (a for _, a in recorded)
+    assert evict[12] == move[6] == plan[12] == 2 and none[12] == 0
+    assert [t.row_bytes for t in evict[11]] == [t.row_bytes for t in move[5]] == [t.row_bytes for t in plan[11]] == [32, 16]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="tensors.*current device"):
+        nms.nms_cache_move_batched(None, n, h, s, budget, iter(rows))
+
+
 def test_binding_refuses_tensors_of_another_device(nms, recorded, monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device"):
