@@ -423,6 +423,19 @@ def test_on_another_stream_in_graphs_and_by_a_plan(nms):
         a.compare(a.wanted())
 
 
+@pytest.mark.parametrize("budget,sums", [(100003, None), (60, None), (1048575, None), (524288, 0.0), (3, float("nan"))])
+def test_the_most_slots(nms, budget, sums):
+    """A frame of NMS_MAX_SLOTS: few moves and as many as there can be, equal sums that no bin parts."""
+    options = {} if sums is None else dict(sums=sums)
+    Cache(nms, 1, 1, 1048576, budget, first=2, recent=min(50, budget), tensors=(rows_of("uint8", 4),), seed=budget, **options).evict()
+
+
+@pytest.mark.parametrize("tokens", [1, 7])
+def test_the_most_frames(nms, tokens):
+    """NMS_MAX_FRAMES frames, with the weights in the launch of the cut (three query rows) and in one of their own (21)."""
+    Cache(nms, 65535, 1, 9, 4, first=1, recent=1, weights=attention(65535, 1, 3, tokens, 9, "bf16", tokens), tensors=(rows_of("uint8", 4),), seed=tokens).evict()
+
+
 def test_two_calls_at_once(nms):
     """Two streams, each with its own buffers and workspace."""
     caches = [Cache(nms, 2, 8, 6000, 1000, 4, 64, weights=attention(2, 8, 2, 4, 6000, "f16", i), tensors=(rows_of("float16", 64),), seed=i) for i in range(2)]

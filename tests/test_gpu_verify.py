@@ -201,6 +201,23 @@ def test_rows_behind_2_to_the_32(nms):
     assert int(tokens[-1, 0]) == 4000000 and int(tokens[:-1].max()) == -1
 
 
+@pytest.mark.parametrize("v,places", [(50, (None, 0, 63, 64, 1023)), (45001, (None, 1023))])
+def test_the_most_drafts(nms, v, places):
+    """NMS_MAX_DRAFTS tokens: with draft and target the same all stand, and refusals at either end of a run of 64 tests."""
+    s, k = len(places), 1024
+    target = torch.softmax(torch.randn((1, 1, v), generator=torch.Generator().manual_seed(v)), -1).expand(s, k + 1, v).clone()
+    drafts = torch.arange(s * k, dtype=torch.int32).view(s, k) % v
+    for i, place in enumerate(places):
+        if place is not None:
+            drafts[i, place] = -1
+    _, accepted = agree(nms, target, target[:, :k], drafts, None, torch.rand((s, k + 1), generator=torch.Generator().manual_seed(1)))
+    assert accepted.tolist() == [k if place is None else place for place in places]
+
+
+def test_the_most_sequences(nms):
+    agree(nms, *inputs(65535, 1, 3, "f32", True, 3)[:3], None, inputs(65535, 1, 3, "f32", True, 3)[3])
+
+
 def test_on_another_stream_in_a_graph_and_by_a_plan(nms):
     target, draft, drafts, u = inputs(6, 3, 20011, "bf16", True, 23)
     want = call(nms, target, draft, drafts, None, u)
