@@ -58,8 +58,8 @@ __global__ void __launch_bounds__(256) cache_move_kernel(MoveArgs a)
 {
     const int frame = blockIdx.y;
     const int2 *list = reinterpret_cast<const int2 *>(a.moves) + (long long)frame * (a.moves_max + 1);
-    const int begin = blockIdx.x * kMoveRows, rows = min(min(list[0].x, a.moves_max) - begin, kMoveRows);
-    if (rows <= 0) return;
+    const int begin = blockIdx.x * kMoveRows, rows = nms_moves_in_stretch(list[0].x, a.moves_max, begin, kMoveRows);
+    if (rows == 0) return;
     if (a.sums != nullptr && threadIdx.x < (unsigned)rows) {
         const int2 pair = list[1 + begin + threadIdx.x];
         const long long base = (long long)frame * a.n_max;

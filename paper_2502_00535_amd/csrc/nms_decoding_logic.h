@@ -33,6 +33,12 @@ NMS_HD int nms_moves_max(int n_max, int budget)
     const int behind = n_max > budget ? n_max - budget : 0;
     return budget < behind ? budget : behind;
 }
+// Moves begin .. begin + most - 1 of a list: how many of them it has.  `count` is what the list says, any number where it comes from elsewhere.
+NMS_HD int nms_moves_in_stretch(int count, int moves_max, int begin, int most)
+{
+    const int all = count < 0 ? 0 : count < moves_max ? count : moves_max;
+    return all <= begin ? 0 : all - begin < most ? all - begin : most;
+}
 static inline size_t nms_decoding_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // ---- eviction: the route ------------------------------------------------------------------------
 // A frame is one workgroup with the keys of all its slots in registers, or (split) is shared by several workgroups in three launches: frames that
