@@ -445,7 +445,7 @@ typedef struct nms_cache_weights {
     const int32_t *valid_tokens;  /* device [sequences]: how many of the query rows count, from the first (clamped to [0, tokens]); NULL: all */
 } nms_cache_weights;
 /* A tensor whose rows move with their slots: row (sequence, head, slot) begins at rows + sequence * sequence_stride +
- * head * head_stride + slot * slot_stride, all in bytes, in any order of size; rows must not overlap.  With pages it begins at rows +
+ * head * head_stride + slot * slot_stride, all in bytes, none below 0, in any order of size; rows must not overlap.  With pages it begins at rows +
  * page * sequence_stride + head * head_stride + (slot % page_slots) * slot_stride, page = table[sequence * table_stride + slot / page_slots].  A page belongs to one
  * sequence: rows of pages that stand twice in the table, or in two sequences' tables, are not moved in any order. */
 typedef struct nms_cache_tensor {
@@ -468,7 +468,8 @@ int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t 
                            int heads, int sequences, const nms_cache_weights *weights, int budget, int first, int recent,
                            uint8_t *keep_out, int32_t *kept_out, int32_t *moves_out, void *workspace, size_t ws_bytes, void *stream);
 /* Moves rows as moves_out of nms_cache_keep_batched says (same n_max, heads, sequences and budget); a pair outside the slots that such a
- * list can name is left out, and so is what lies behind its nms_cache_moves_max entries; a number of moves below 0 is 0.  `tensors` is a HOST array of n_tensors <= NMS_CACHE_MAX_TENSORS, `pages` a HOST pointer or NULL. */
+ * list can name is left out, and so is what lies behind its nms_cache_moves_max entries; a number of moves below 0 is 0.  `tensors`
+ * is a HOST array of n_tensors <= NMS_CACHE_MAX_TENSORS, `pages` a HOST pointer or NULL. */
 int nms_cache_move_batched(const int32_t *moves, int n_max, int heads, int sequences, int budget, const nms_cache_tensor *tensors,
                            int n_tensors, const nms_cache_pages *pages, void *stream);
 int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *counts, const int32_t *lengths, int n_max,

@@ -95,8 +95,11 @@ int tensors_status(const nms_cache_tensor *tensors, int n_tensors, const nms_cac
 {
     if (n_tensors < 0 || (n_tensors > 0 && tensors == nullptr)) return NMS_ERR_INVALID_ARG;
     if (n_tensors > NMS_CACHE_MAX_TENSORS) return NMS_ERR_TOO_LARGE;
-    for (int i = 0; i < n_tensors; ++i)
-        if (tensors[i].rows == nullptr || tensors[i].row_bytes < 1 || tensors[i].row_bytes > (1 << 20)) return NMS_ERR_INVALID_ARG;
+    for (int i = 0; i < n_tensors; ++i) {
+        const nms_cache_tensor &t = tensors[i];
+        if (t.rows == nullptr || t.row_bytes < 1 || t.row_bytes > (1 << 20)) return NMS_ERR_INVALID_ARG;
+        if (t.sequence_stride < 0 || t.head_stride < 0 || t.slot_stride < 0) return NMS_ERR_INVALID_ARG;  // an offset below 0 stands for a bad page
+    }
     if (pages == nullptr) return NMS_OK;
     if (pages->table == nullptr || pages->page_slots < 1 || pages->pages < 0 || pages->reserved != 0) return NMS_ERR_INVALID_ARG;
     return (long long)pages->table_stride * pages->page_slots < n_max ? NMS_ERR_INVALID_ARG : NMS_OK;
