@@ -396,7 +396,8 @@ enum { NMS_TYPE_F32 = 0, NMS_TYPE_F16 = 1, NMS_TYPE_BF16 = 2 };
  *   counts   [sequences] int32, values above drafts_max count as drafts_max; NULL: drafts_max everywhere.  Below 0: no
  *            sequence at this place of the batch: nothing of it is read, accepted_out 0, tokens -1
  *   uniforms [sequences][drafts_max + 1] float: drafts_max for the tests, the last for the token
- *   tokens_out [sequences][drafts_max + 1] int32, accepted_out [sequences] int32
+ *   tokens_out [sequences][drafts_max + 1] int32, accepted_out [sequences] int32; neither may overlap drafts, counts, uniforms or the
+ *            other (else NMS_ERR_INVALID_ARG)
  *   workspace  >= nms_verify_workspace_bytes(vocabulary, sequences) bytes, 256-byte aligned; may be NULL when that is 0
  * sequences == 0 is NMS_OK; vocabulary must be at least 1, strides at least vocabulary.
  */
@@ -428,11 +429,11 @@ int nms_verify_batched(const void *target, long long target_stride, const void *
  *   weights    HOST pointer, or NULL (nothing is added)
  *   keep_out   [sequences][heads][n_max] bytes, 1 = the row of this slot stays (slots as before any move), 0 = it goes or
  *              there is none; NULL: not wanted
- *   kept_out   [sequences] int32, k: the next step's rows are written behind it (a buffer other than counts, lengths and
- *              valid_tokens: else NMS_ERR_INVALID_ARG); NULL: not wanted
+ *   kept_out   [sequences] int32, k: the next step's rows are written behind it; NULL: not wanted
  *   moves_out  int32 [sequences][heads][nms_cache_moves_max(n_max, budget) + 1][2]: the number of moves and 0, then pairs
  *              (to, from), to ascending, from ascending; entries behind them are left as they are; NULL: not wanted
  *   workspace  >= nms_cache_workspace_bytes(n_max, heads, sequences, budget) bytes, 256-byte aligned
+ * No buffer that is written may overlap counts, lengths or valid_tokens (else NMS_ERR_INVALID_ARG).
  * n_max <= NMS_MAX_SLOTS, sequences * heads <= NMS_MAX_FRAMES, group * tokens <= NMS_MAX_QUERY_ROWS; budget, first and recent >= 0.
  */
 typedef struct nms_cache_weights {

@@ -85,10 +85,18 @@ int weights_status(const nms_cache_weights *w)
     return NMS_OK;
 }
 
-// kept_out is written while other workgroups still read these.
-bool overwrites(const int32_t *kept, const int32_t *counts, const int32_t *lengths, const nms_cache_weights *w)
+// The numbers of a sequence are read by every workgroup of its heads, and some have written what they have to write by then.
+bool overwrites(const CacheArgs &a, const nms_cache_weights *w, int heads, int sequences, bool positions_too)
 {
-    return kept != nullptr && (kept == counts || kept == lengths || (w != nullptr && kept == w->valid_tokens));
+    const size_t slots = (size_t)heads * sequences * a.n_max, each = (size_t)sequences * sizeof(int32_t);
+    const size_t moves = (size_t)heads * sequences * ((size_t)a.moves_max + 1) * 2 * sizeof(int32_t);
+    const NmsBuffer written[] = {{a.sums, slots * sizeof(float)}, {positions_too ? a.positions : nullptr, slots * sizeof(int32_t)}, {a.keep, slots},
+                                 {a.kept, each}, {a.moves, moves}};
+    const NmsBuffer read[] = {{a.counts, each}, {a.lengths, each}, {w != nullptr ? w->valid_tokens : nullptr, each}};
+    for (const NmsBuffer &out : written)
+        for (const NmsBuffer &in : read)
+            if (nms_overlap(out, in)) return true;
+    return false;
 }
 
 int tensors_status(const nms_cache_tensor *tensors, int n_tensors, const nms_cache_pages *pages, int n_max)
@@ -236,6 +244,11 @@ int nms_verify_batched(const void *target, long long target_stride, const void *
     if (sequences == 0) return NMS_OK;
     if (target == nullptr || (drafts == nullptr && drafts_max > 0) || uniforms == nullptr || tokens_out == nullptr || accepted_out == nullptr)
         return NMS_ERR_INVALID_ARG;
+    const size_t each = (size_t)sequences * sizeof(int32_t);
+    const NmsBuffer out[] = {{tokens_out, each * (drafts_max + 1)}, {accepted_out, each}};  // written while other sequences' inputs are read
+    for (const NmsBuffer &in : {NmsBuffer{drafts, each * drafts_max}, NmsBuffer{counts, each}, NmsBuffer{uniforms, each * (drafts_max + 1)}})
+        if (nms_overlap(out[0], in) || nms_overlap(out[1], in)) return NMS_ERR_INVALID_ARG;
+    if (nms_overlap(out[0], out[1])) return NMS_ERR_INVALID_ARG;
     const int st = workspace_status(workspace, ws_bytes, nms_verify_workspace_bytes(vocabulary, sequences));
     if (st != NMS_OK) return st;
     const VerifyArgs a = {target, draft, target_stride, draft_stride, drafts, counts, uniforms, tokens_out, accepted_out, drafts_max, vocabulary};
@@ -267,11 +280,11 @@ int nms_cache_keep_batched(float *sums, const int32_t *positions, const int32_t 
     st = weights_status(weights);
     if (st != NMS_OK) return st;
     if (n_max == 0 || heads == 0 || sequences == 0) return NMS_OK;
-    if (sums == nullptr || overwrites(kept_out, counts, lengths, weights)) return NMS_ERR_INVALID_ARG;
-    st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
-    if (st != NMS_OK) return st;
     const CacheArgs a = {sums, const_cast<int32_t *>(positions), counts, lengths, keep_out, kept_out, moves_out, n_max, heads, budget, first, recent,
                          nms_moves_max(n_max, budget), false};
+    if (sums == nullptr || overwrites(a, weights, heads, sequences, false)) return NMS_ERR_INVALID_ARG;
+    st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
+    if (st != NMS_OK) return st;
     return keep_and_move(a, weights, MoveArgs{}, workspace, heads * sequences, static_cast<hipStream_t>(stream));
 }
 
@@ -300,15 +313,14 @@ int nms_cache_evict_batched(float *sums, int32_t *positions, const int32_t *coun
     st = tensors_status(tensors, n_tensors, pages, n_max);
     if (st != NMS_OK) return st;
     if (n_max == 0 || heads == 0 || sequences == 0) return NMS_OK;
-    if (sums == nullptr || overwrites(kept_out, counts, lengths, weights)) return NMS_ERR_INVALID_ARG;
+    CacheArgs a = {sums, positions, counts, lengths, keep_out, kept_out, nullptr, n_max, heads, budget, first, recent, nms_moves_max(n_max, budget), true};
+    if (sums == nullptr || overwrites(a, weights, heads, sequences, true)) return NMS_ERR_INVALID_ARG;
     st = workspace_status(workspace, ws_bytes, nms_cache_workspace_bytes(n_max, heads, sequences, budget));
     if (st != NMS_OK) return st;
     const int frames = heads * sequences;
     // the list of moves first, then what finds it
-    int32_t *moves = static_cast<int32_t *>(workspace);
+    int32_t *moves = a.moves = static_cast<int32_t *>(workspace);
     void *scratch = static_cast<char *>(workspace) + nms_cache_list_bytes(n_max, frames, budget);
-    const CacheArgs a = {sums, positions, counts, lengths, keep_out, kept_out, moves, n_max, heads, budget, first, recent,
-                         nms_moves_max(n_max, budget), true};
     return keep_and_move(a, weights, move_args(moves, n_max, heads, budget, tensors, n_tensors, pages), scratch, frames, static_cast<hipStream_t>(stream));
 }
 

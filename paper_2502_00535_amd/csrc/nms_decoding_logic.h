@@ -117,6 +117,17 @@ static inline size_t nms_verify_scratch(int vocabulary, int sequences)
     return nms_verify_sums_bytes(vocabulary, sequences) + nms_decoding_align256((size_t)sequences * 2 * sizeof(int32_t));
 }
 
+// ---- buffers ------------------------------------------------------------------------------------
+struct NmsBuffer {
+    const void *at;   // nullptr: not given
+    size_t bytes;
+};
+static inline bool nms_overlap(const NmsBuffer &a, const NmsBuffer &b)
+{
+    const uintptr_t i = (uintptr_t)a.at, j = (uintptr_t)b.at;
+    return i != 0 && j != 0 && (i < j ? j - i < a.bytes : i - j < b.bytes) && a.bytes > 0 && b.bytes > 0;
+}
+
 // ---- addresses ----------------------------------------------------------------------------------
 // Byte offset of row (sequence, head, slot), or -1 when its page is none of the tensor's.
 NMS_HD long long nms_cache_row_offset(const nms_cache_tensor &t, const nms_cache_pages &pages, int sequence, int head, int slot)

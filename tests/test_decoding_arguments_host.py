@@ -44,3 +44,53 @@ def test_strides_below_0_are_refused(nms):
                 assert nms.lib.nms_cache_evict_batched(p, p, None, None, 50, 2, 3, None, 10, 0, 4, tensors, many, pg, None, None, None, 0,
                                                        None) == nms.NMS_ERR_INVALID_ARG, strides
                 assert nms.lib.nms_cache_move_batched(p, 0, 2, 3, 10, tensors, many, pg, None) == nms.NMS_ERR_INVALID_ARG, strides
+
+
+def test_outputs_of_verification_overlap_nothing(nms):
+    """A workgroup writes its sequence's outputs while others still read their inputs.  (The workspace is too small in these calls, and that is looked at
+    after the buffers.)"""
+    k, v, s = 3, 50000, 6
+    assert nms.nms_verify_workspace_bytes(v, s) > 0
+    places = dict(drafts=0x10000, counts=0x20000, uniforms=0x30000, tokens=0x40000, accepted=0x50000)
+    sizes = dict(drafts=4 * s * k, counts=4 * s, uniforms=4 * s * (k + 1), tokens=4 * s * (k + 1), accepted=4 * s)
+
+    def call(**at):
+        a = {name: ctypes.c_void_p(place) for name, place in {**places, **at}.items()}
+        return nms.lib.nms_verify_batched(P, v, None, v, 0, a["drafts"], a["counts"], k, v, s, a["uniforms"], a["tokens"], a["accepted"], None, 0, None)
+    assert call() == call(counts=None) == nms.NMS_ERR_WORKSPACE
+    for out in ("tokens", "accepted"):
+        for other in places:
+            if other == out:
+                continue
+            begin, end = places[other] - sizes[out], places[other] + sizes[other]
+            for at in (begin + 4, places[other], end - 4):
+                assert call(**{out: at}) == nms.NMS_ERR_INVALID_ARG, (out, other, at)
+            for at in (begin, end):
+                assert call(**{out: at}) == nms.NMS_ERR_WORKSPACE, (out, other, at)
+
+
+def test_outputs_of_eviction_overlap_no_number_of_a_sequence(nms):
+    """counts, lengths and valid_tokens are read by every head's workgroup, and some of them have written their outputs by then."""
+    n, h, s, budget = 50, 2, 6, 10
+    places = dict(sums=0x100000, positions=0x200000, keep=0x300000, kept=0x400000, moves=0x500000)
+    sizes = dict(sums=4 * s * h * n, positions=4 * s * h * n, keep=s * h * n, kept=4 * s, moves=8 * s * h * (nms.nms_cache_moves_max(n, budget) + 1))
+
+    def call(whole, counts=None, lengths=None, valid=None):
+        w = nms.NmsCacheWeights(P, n, 0, 1, 1, n, valid)
+        a = {name: ctypes.c_void_p(place) for name, place in places.items()}
+        if whole:
+            return nms.lib.nms_cache_evict_batched(a["sums"], a["positions"], counts, lengths, n, h, s, w, budget, 0, 4, None, 0, None, a["keep"],
+                                                   a["kept"], None, 0, None)
+        return nms.lib.nms_cache_keep_batched(a["sums"], a["positions"], counts, lengths, n, h, s, w, budget, 0, 4, a["keep"], a["kept"],
+                                              a["moves"], None, 0, None)
+    for whole in (True, False):
+        assert call(whole) == nms.NMS_ERR_WORKSPACE
+        for name in ("counts", "lengths", "valid"):
+            for out in places:
+                if out == ("moves" if whole else "positions"):   # the whole path has no list, the other call only reads positions
+                    continue
+                begin, end = places[out] - 4 * s, places[out] + sizes[out]
+                for at in (begin + 4, places[out], end - 4):
+                    assert call(whole, **{name: at}) == nms.NMS_ERR_INVALID_ARG, (name, out, at)
+                for at in (begin, end):
+                    assert call(whole, **{name: at}) == nms.NMS_ERR_WORKSPACE, (name, out, at)
