@@ -572,6 +572,14 @@ NMS_MAX_FRAMES, NMS_MAX_DRAFTS, NMS_MAX_VOCABULARY, NMS_MAX_SLOTS, NMS_CACHE_MAX
 _TYPES = {torch.float32: NMS_TYPE_F32, torch.float16: NMS_TYPE_F16, torch.bfloat16: NMS_TYPE_BF16}
 
 
+def _int(value, what):
+    """A number as the C ABI takes it: ctypes keeps the low 32 bits of a larger one without a word."""
+    v = int(value)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{what}: {v} does not fit 32 bits")
+    return v
+
+
 def _here(*named):
     """The kernels run on the current device: tensors of another one are refused.  (name, tensor) in turn."""
     device = torch.cuda.current_device()
@@ -622,11 +630,11 @@ def _rows(t, shape, what):
 
 
 def nms_verify_workspace_bytes(vocabulary: int, sequences: int) -> int:
-    return int(lib.nms_verify_workspace_bytes(int(vocabulary), int(sequences)))
+    return int(lib.nms_verify_workspace_bytes(_int(vocabulary, "vocabulary"), _int(sequences, "sequences")))
 
 
 def _verify_arguments(target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace):
-    k, v, s = int(drafts_max), int(vocabulary), int(sequences)
+    k, v, s = _int(drafts_max, "drafts_max"), _int(vocabulary, "vocabulary"), _int(sequences, "sequences")
     _here("target", target, "draft", draft, "drafts", drafts, "counts", counts, "uniforms", uniforms, "tokens_out", tokens_out,
           "accepted_out", accepted_out, "workspace", workspace)
     t_at, t_row, d_at, d_row, kind = None, v, None, v, NMS_TYPE_F32
@@ -653,11 +661,15 @@ def nms_verify_batched(target, draft, drafts, counts, drafts_max, vocabulary, se
 
 
 def nms_cache_moves_max(n_max: int, budget: int) -> int:
-    return int(lib.nms_cache_moves_max(int(n_max), int(budget)))
+    return int(lib.nms_cache_moves_max(_int(n_max, "n_max"), _int(budget, "budget")))
 
 
 def nms_cache_workspace_bytes(n_max: int, heads: int, sequences: int, budget: int) -> int:
-    return int(lib.nms_cache_workspace_bytes(int(n_max), int(heads), int(sequences), int(budget)))
+    return int(lib.nms_cache_workspace_bytes(*_cache_sizes(n_max, heads, sequences, budget)))
+
+
+def _cache_sizes(n_max, heads, sequences, budget):
+    return _int(n_max, "n_max"), _int(heads, "heads"), _int(sequences, "sequences"), _int(budget, "budget")
 
 
 def _cache_elements(n_max, heads, sequences):
@@ -675,7 +687,8 @@ def _cache_weights(weights, valid_tokens, heads, sequences):
     if len(shape) != 5 or shape[0] != sequences or shape[1] != heads:
         raise ValueError(f"weights: shape {shape}, the call needs ({sequences}, {heads}, group, tokens, columns)")
     at, row = _rows(weights, shape, "weights")
-    return NmsCacheWeights(at, row, _type_of(weights, "weights"), shape[2], shape[3], shape[4],
+    group, tokens, columns = (_int(x, "weights") for x in shape[2:])
+    return NmsCacheWeights(at, row, _type_of(weights, "weights"), group, tokens, columns,
                            _ptr(valid_tokens, "int32", "valid_tokens", sequences))
 
 
@@ -718,14 +731,15 @@ def _cache_tensors(tensors, n_max, heads, sequences, page_table):
     each = -(-max(n_max, 0) // max(slots, 1))
     if page_table.shape[1] < each:
         raise ValueError(f"page_table: {page_table.shape[1]} pages to a sequence, the call needs {each}")
-    return structs, len(tensors), NmsCachePages(_ptr(page_table, "int32", "page_table", 0), page_table.shape[1], slots, count, 0)
+    return structs, len(tensors), NmsCachePages(_ptr(page_table, "int32", "page_table", 0), _int(page_table.shape[1], "page_table"),
+                                                  _int(slots, "tensors"), _int(count, "tensors"), 0)
 
 
 def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, keep_out, kept_out, moves_out,
                            workspace, weights=None, valid_tokens=None, stream=None):
     """weights: [sequences, heads, group, tokens, columns], rows at one distance from each other, or None.
     moves_out: at least sequences * heads * (nms_cache_moves_max(n_max, budget) + 1) * 2 elements, or None."""
-    n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
+    n, h, s, b = _cache_sizes(n_max, heads, sequences, budget)
     _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
           "moves_out", moves_out, "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens)
     all_, s_ = _cache_elements(n, h, s)
@@ -733,8 +747,8 @@ def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, seque
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
     _check(lib.nms_cache_keep_batched(
         _ptr(sums, "float32", "sums", all_), _ptr(positions, "int32", "positions", all_), _ptr(counts, "int32", "counts", s_),
-        _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, int(first), int(recent), _ptr(keep_out, "uint8", "keep_out", all_),
-        _ptr(kept_out, "int32", "kept_out", s_),
+        _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, _int(first, "first"), _int(recent, "recent"),
+        _ptr(keep_out, "uint8", "keep_out", all_), _ptr(kept_out, "int32", "kept_out", s_),
         _ptr(moves_out, "int32", "moves_out", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ else 0), w, wb, _stream(stream)),
         "nms_cache_keep_batched")
 
@@ -742,7 +756,7 @@ def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, seque
 def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page_table=None, stream=None):
     """tensors: up to eight of shape [sequences, heads, n_max, row ...] (any strides whose rows are whole), or with a page table
     ([sequences, pages of a sequence] int32) [pages, heads, slots of a page, row ...]."""
-    n, h, s, b = int(n_max), int(heads), int(sequences), int(budget)
+    n, h, s, b = _cache_sizes(n_max, heads, sequences, budget)
     tensors = tuple(tensors or ())  # gone over more than once
     _here("moves", moves, "page_table", page_table, *(x for t in tensors for x in ("tensors", t)))
     all_, s_ = _cache_elements(n, h, s)
@@ -753,7 +767,7 @@ def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page
 
 def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
                      workspace, weights, valid_tokens, page_table):
-    n, h, s = int(n_max), int(heads), int(sequences)
+    n, h, s, b = _cache_sizes(n_max, heads, sequences, budget)
     tensors = tuple(tensors or ())  # gone over more than once
     _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
           "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens, "page_table", page_table,
@@ -763,7 +777,7 @@ def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, 
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
     structs, many, pages = _cache_tensors(tensors if all_ else (), n, h, s, page_table)
     return (_ptr(sums, "float32", "sums", all_), _ptr(positions, "int32", "positions", all_), _ptr(counts, "int32", "counts", s_),
-            _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, int(budget), int(first), int(recent), structs, many, pages,
+            _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, _int(first, "first"), _int(recent, "recent"), structs, many, pages,
             _ptr(keep_out, "uint8", "keep_out", all_), _ptr(kept_out, "int32", "kept_out", s_), w, wb)
 
 

@@ -4,20 +4,12 @@ import os
 import subprocess
 
 import pytest
+import torch
+
+from test_decoding_host import gpu, nms, recorded  # noqa: F401  (fixtures, and CPU tensors that say they lie on the GPU)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 P = 0x1000          # an address that nothing looks at
-
-
-@pytest.fixture(scope="module")
-def nms():
-    from paper_2502_00535_amd import build as nms_build
-
-    if nms_build.is_stale():
-        nms_build.build_library()
-    import paper_2502_00535_amd.binding as binding
-
-    return binding
 
 
 def test_a_list_may_say_any_number_of_moves(tmp_path):
@@ -94,3 +86,47 @@ def test_outputs_of_eviction_overlap_no_number_of_a_sequence(nms):
                     assert call(whole, **{name: at}) == nms.NMS_ERR_INVALID_ARG, (name, out, at)
                 for at in (begin, end):
                     assert call(whole, **{name: at}) == nms.NMS_ERR_WORKSPACE, (name, out, at)
+
+
+BEYOND = (2 ** 32, -2 ** 32, 2 ** 31, -2 ** 31 - 2 ** 20, 2 ** 64)  # and stay beyond when a size is added
+
+
+@pytest.mark.parametrize("beyond", BEYOND)
+def test_numbers_beyond_32_bits_are_refused(nms, recorded, beyond):
+    """Not taken by their low 32 bits: a budget of 2^32 + 16 is not 16, and 2^32 + 40 slots are not 40 of buffers that nobody has looked at."""
+    n, h, s, budget = 40, 2, 3, 16
+    i32 = torch.int32
+    cache = dict(sums=gpu(s, h, n), positions=None, counts=None, lengths=None, n_max=n, heads=h, sequences=s, budget=budget, first=0, recent=0,
+                 keep_out=None, kept_out=None, workspace=gpu(1 << 16, dtype=torch.uint8))
+    move = dict(moves=gpu(s * h * (budget + 1) * 2, dtype=i32), n_max=n, heads=h, sequences=s, budget=budget, tensors=[gpu(s, h, n, 4)])
+    verify = dict(target=gpu(s, 3, 50), draft=None, drafts=gpu(s, 2, dtype=i32), counts=None, drafts_max=2, vocabulary=50, sequences=s,
+                  uniforms=gpu(s, 3), tokens_out=gpu(s, 3, dtype=i32), accepted_out=gpu(s, dtype=i32), workspace=gpu(4096, dtype=torch.uint8))
+    calls = [(nms.nms_cache_evict_batched, {**cache, "tensors": []}, ("n_max", "heads", "sequences", "budget", "first", "recent")),
+             (nms.CachePlan, {**cache, "tensors": []}, ("n_max", "heads", "sequences", "budget", "first", "recent")),
+             (nms.nms_cache_keep_batched, {**cache, "moves_out": None}, ("n_max", "heads", "sequences", "budget", "first", "recent")),
+             (nms.nms_cache_move_batched, move, ("n_max", "heads", "sequences", "budget")),
+             (nms.nms_verify_batched, verify, ("drafts_max", "vocabulary", "sequences")), (nms.VerifyPlan, verify, ("drafts_max", "vocabulary", "sequences"))]
+    for call, good, names in calls:
+        call(**good)
+        before = len(recorded)
+        for name in names:
+            with pytest.raises(ValueError, match=name):
+                call(**{**good, name: beyond + good[name]})
+        assert len(recorded) == before
+    for size, good in ((nms.nms_cache_moves_max, (n, budget)), (nms.nms_cache_workspace_bytes, (n, h, s, budget)), (nms.nms_verify_workspace_bytes, (50, s))):
+        for i in range(len(good)):
+            with pytest.raises(ValueError):
+                size(*good[:i], good[i] + beyond, *good[i + 1:])
+
+
+def test_dimensions_beyond_32_bits_are_refused(nms, recorded):
+    """Tensors of nothing can have any shape."""
+    n, h, s = 40, 1, 1
+    rest = (gpu(s, h, n), None, None, None, n, h, s, 16, 0, 0)
+    after = (None, None, gpu(1 << 16, dtype=torch.uint8))
+    for group, tokens, columns in ((2 ** 32 + 1, 1, 0), (1, 2 ** 32 + 1, 0), (1, 0, 2 ** 32 + n)):
+        with pytest.raises(ValueError, match="weights"):
+            nms.nms_cache_evict_batched(*rest, [], *after, weights=gpu(s, h, group, tokens, columns))
+    with pytest.raises(ValueError, match="page_table|tensors"):
+        nms.nms_cache_evict_batched(*rest, [gpu(2 ** 32 + 9, h, 16, 0)], *after, page_table=gpu(s, 3, dtype=torch.int32))
+    assert not recorded
