@@ -792,12 +792,16 @@ def nms_cache_evict_batched(sums, positions, counts, lengths, n_max, heads, sequ
 class _DecodingPlan:
     """A call with its arguments marshalled once, for decoding loops whose buffers stay: each call is then a single foreign call.
     The plan holds references to its tensors; a call uses the stream given here, or the current one of the device that the plan was
-    made on, which must be the current device."""
+    made on; while another one is current it is refused."""
 
     def __init__(self, entry, args, keepalive, stream):
         self._entry, self._fn, self._args, self._keepalive, self._given = entry, getattr(lib, entry), args, keepalive, stream
+        self._current = _current_device if _current_device is not None and torch.cuda.is_initialized() else lambda: torch.cuda.current_device()
+        self._device = self._current()
 
     def __call__(self):
+        if self._current() != self._device:
+            raise ValueError(f"{self._entry}: the plan was made on cuda:{self._device}, the current device is cuda:{self._current()}")
         status = self._fn(*self._args, _stream(self._given))
         if status != NMS_OK:
             raise NmsError(status, self._entry)

@@ -130,3 +130,18 @@ def test_dimensions_beyond_32_bits_are_refused(nms, recorded):
     with pytest.raises(ValueError, match="page_table|tensors"):
         nms.nms_cache_evict_batched(*rest, [gpu(2 ** 32 + 9, h, 16, 0)], *after, page_table=gpu(s, 3, dtype=torch.int32))
     assert not recorded
+
+
+def test_a_plan_is_called_on_its_own_device(nms, recorded, monkeypatch):
+    """Its kernels would run on the current device otherwise, with addresses of another one."""
+    n, h, s, budget = 40, 2, 3, 16
+    cache = nms.CachePlan(gpu(s, h, n), None, None, None, n, h, s, budget, 0, 0, [], None, None, gpu(1 << 16, dtype=torch.uint8))
+    verify = nms.VerifyPlan(gpu(1, 1, 9), None, None, None, 0, 9, 1, gpu(1, 1), gpu(1, 1, dtype=torch.int32), gpu(1, dtype=torch.int32), None)
+    cache(), verify()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for plan in (cache, verify):
+        with pytest.raises(ValueError, match="cuda:0.*cuda:1"):
+            plan()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    cache(), verify()
+    assert len(recorded) == 4
