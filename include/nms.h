@@ -394,7 +394,8 @@ enum { NMS_TYPE_F32 = 0, NMS_TYPE_F16 = 1, NMS_TYPE_BF16 = 2 };
  *            tokens alone, q_i is 1 at x_i and 0 elsewhere
  *   drafts   [sequences][drafts_max] int32 (may be NULL when drafts_max is 0: a plain draw from one row)
  *   counts   [sequences] int32, values above drafts_max count as drafts_max; NULL: drafts_max everywhere.  Below 0: no
- *            sequence at this place of the batch: nothing of it is read, accepted_out 0, tokens -1
+ *            sequence at this place of the batch: accepted_out 0, tokens -1.  Its rows of target and draft are not read; its
+ *            drafts and uniforms may be, whatever they hold (as may those behind a count)
  *   uniforms [sequences][drafts_max + 1] float: drafts_max for the tests, the last for the token
  *   tokens_out [sequences][drafts_max + 1] int32, accepted_out [sequences] int32; neither may overlap drafts, counts, uniforms or the
  *            other (else NMS_ERR_INVALID_ARG)

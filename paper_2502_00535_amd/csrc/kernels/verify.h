@@ -31,8 +31,9 @@ struct VerifyArgs {
     int drafts_max, vocabulary;
 };
 
-// How many drafted tokens of the sequence stand, by one wavefront (every lane gets the answer): 64 tests at a time.  Loads do not wait for
-// the count: it is a chain of three (token, its two probabilities, the row) as it is.
+// How many drafted tokens of the sequence stand, by one wavefront (every lane gets the answer): 64 tests at a time.  Tokens and random
+// numbers are loaded beside the count, not after it, also where it then says that there is no sequence: it is a chain of three (token, its two
+// probabilities, the row) as it is.
 template <typename T, bool kDraft>
 __device__ __forceinline__ int count_accepted(const VerifyArgs &a, int s, int lane, int &count)
 {
