@@ -446,11 +446,11 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
         else load(std::false_type{});
     }
     // which rows stay, a bit to an element
-    using Bits = typename std::conditional<(kEach > 32), unsigned long long, uint32_t>::type;
-    Bits stay = 0;
+    static_assert(kEach <= 32, "one word of bits");
+    uint32_t stay = 0;
     if (k == n) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] != 0u) << e;
+        for (int e = 0; e < kEach; ++e) stay |= (uint32_t)(key[e] != 0u) << e;
     } else if (k > 0) {
         uint32_t lo = 0, hi = 0, need = (uint32_t)k, left = (uint32_t)n;
         if (one_goes) {
@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
             cut = find_cut<kVecs>(room, key, lo, hi, need, left, log_bins, wave, lane);
             const bool ties = cut.wanted < cut.there;
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) stay |= (Bits)(key[e] > cut.key || (key[e] == cut.key && !ties)) << e;
+            for (int e = 0; e < kEach; ++e) stay |= (uint32_t)(key[e] > cut.key || (key[e] == cut.key && !ties)) << e;
             if (!ties) break;
             // of the rows with that key the lowest slots: once more, with the complements of their slots for keys (no two are the same)
 #pragma unroll
@@ -494,14 +494,14 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
     // moves: slots below k whose row goes are free, rows that stay beyond take them in order
     uint32_t total = 0;
     if (a.moves_max > 0 && (a.moves != nullptr || a.move_sums)) {
-        Bits is_free = 0, moves = 0;
+        uint32_t is_free = 0, moves = 0;
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const bool s = stay >> e & 1, low = slot_of(e) < k;
-            is_free |= (Bits)(low && !s) << e;
-            moves |= (Bits)(!low && s) << e;
+            is_free |= (uint32_t)(low && !s) << e;
+            moves |= (uint32_t)(!low && s) << e;
         }
-        const uint32_t counts = wave_running_count((uint32_t)__popcll(is_free) << 16 | (uint32_t)__popcll(moves));  // at most 2048 of each in a wavefront
+        const uint32_t counts = wave_running_count((uint32_t)__popc(is_free) << 16 | (uint32_t)__popc(moves));  // at most 2048 of each in a wavefront
         if (lane == 63) room.wave_b[wave] = counts;
         __syncthreads();
         uint32_t to = 0, from = 0;
@@ -512,10 +512,10 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
             total += c & 0xffffu;
         }
         // in order of slots: visit(element, its rank) for each of the flagged
-        auto ranked = [&](Bits flags, uint32_t rank0, auto &&visit) {
+        auto ranked = [&](uint32_t flags, uint32_t rank0, auto &&visit) {
 #pragma unroll
             for (int v = 0; v < kVecs; ++v) {
-                const uint32_t own = (uint32_t)(flags >> (v * 4)) & 15u;
+                const uint32_t own = flags >> (v * 4) & 15u;
                 if (__ballot(own != 0) == 0) continue;
                 const uint32_t upto = wave_running_count(__popc(own));
                 uint32_t rank = rank0 + upto - __popc(own);
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kKeepMaxWaves * 64) cache_keep_kernel(CacheArg
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
         const int i = base_slot + v * 256;
-        const uint32_t flags = (uint32_t)(stay >> (v * 4)) & 15u;
+        const uint32_t flags = stay >> (v * 4) & 15u;
         if (a.keep != nullptr) {
             Four<uint8_t> f;
 #pragma unroll
