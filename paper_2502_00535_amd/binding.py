@@ -572,12 +572,12 @@ NMS_MAX_FRAMES, NMS_MAX_DRAFTS, NMS_MAX_VOCABULARY, NMS_MAX_SLOTS, NMS_CACHE_MAX
 _TYPES = {torch.float32: NMS_TYPE_F32, torch.float16: NMS_TYPE_F16, torch.bfloat16: NMS_TYPE_BF16}
 
 
-def _int(value, what):
-    """A number as the C ABI takes it: ctypes keeps the low 32 bits of a larger one without a word."""
-    v = int(value)
-    if not -2 ** 31 <= v < 2 ** 31:
-        raise ValueError(f"{what}: {v} does not fit 32 bits")
-    return v
+def _beyond_32_bits(**named):
+    """ctypes keeps the low 32 bits of a larger number without a word.  For numbers of which one is below 0 or does not fit: the former are the
+    library's to refuse."""
+    for what, v in named.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{what}: {v} does not fit 32 bits")
 
 
 def _here(*named):
@@ -630,11 +630,16 @@ def _rows(t, shape, what):
 
 
 def nms_verify_workspace_bytes(vocabulary: int, sequences: int) -> int:
-    return int(lib.nms_verify_workspace_bytes(_int(vocabulary, "vocabulary"), _int(sequences, "sequences")))
+    v, s = int(vocabulary), int(sequences)
+    if (v | s) >> 31:
+        _beyond_32_bits(vocabulary=v, sequences=s)
+    return int(lib.nms_verify_workspace_bytes(v, s))
 
 
 def _verify_arguments(target, draft, drafts, counts, drafts_max, vocabulary, sequences, uniforms, tokens_out, accepted_out, workspace):
-    k, v, s = _int(drafts_max, "drafts_max"), _int(vocabulary, "vocabulary"), _int(sequences, "sequences")
+    k, v, s = int(drafts_max), int(vocabulary), int(sequences)
+    if (k | v | s) >> 31:
+        _beyond_32_bits(drafts_max=k, vocabulary=v, sequences=s)
     _here("target", target, "draft", draft, "drafts", drafts, "counts", counts, "uniforms", uniforms, "tokens_out", tokens_out,
           "accepted_out", accepted_out, "workspace", workspace)
     t_at, t_row, d_at, d_row, kind = None, v, None, v, NMS_TYPE_F32
@@ -661,15 +666,21 @@ def nms_verify_batched(target, draft, drafts, counts, drafts_max, vocabulary, se
 
 
 def nms_cache_moves_max(n_max: int, budget: int) -> int:
-    return int(lib.nms_cache_moves_max(_int(n_max, "n_max"), _int(budget, "budget")))
+    n, b = int(n_max), int(budget)
+    if (n | b) >> 31:
+        _beyond_32_bits(n_max=n, budget=b)
+    return int(lib.nms_cache_moves_max(n, b))
 
 
 def nms_cache_workspace_bytes(n_max: int, heads: int, sequences: int, budget: int) -> int:
-    return int(lib.nms_cache_workspace_bytes(*_cache_sizes(n_max, heads, sequences, budget)))
+    return int(lib.nms_cache_workspace_bytes(*_cache_sizes(n_max, heads, sequences, budget)[:4]))
 
 
-def _cache_sizes(n_max, heads, sequences, budget):
-    return _int(n_max, "n_max"), _int(heads, "heads"), _int(sequences, "sequences"), _int(budget, "budget")
+def _cache_sizes(n_max, heads, sequences, budget, first=0, recent=0):
+    n, h, s, b, f, r = int(n_max), int(heads), int(sequences), int(budget), int(first), int(recent)
+    if (n | h | s | b | f | r) >> 31:
+        _beyond_32_bits(n_max=n, heads=h, sequences=s, budget=b, first=f, recent=r)
+    return n, h, s, b, f, r
 
 
 def _cache_elements(n_max, heads, sequences):
@@ -687,8 +698,9 @@ def _cache_weights(weights, valid_tokens, heads, sequences):
     if len(shape) != 5 or shape[0] != sequences or shape[1] != heads:
         raise ValueError(f"weights: shape {shape}, the call needs ({sequences}, {heads}, group, tokens, columns)")
     at, row = _rows(weights, shape, "weights")
-    group, tokens, columns = (_int(x, "weights") for x in shape[2:])
-    return NmsCacheWeights(at, row, _type_of(weights, "weights"), group, tokens, columns,
+    if (shape[2] | shape[3] | shape[4]) >> 31:
+        raise ValueError(f"weights: shape {shape} does not fit 32 bits")
+    return NmsCacheWeights(at, row, _type_of(weights, "weights"), shape[2], shape[3], shape[4],
                            _ptr(valid_tokens, "int32", "valid_tokens", sequences))
 
 
@@ -731,15 +743,16 @@ def _cache_tensors(tensors, n_max, heads, sequences, page_table):
     each = -(-max(n_max, 0) // max(slots, 1))
     if page_table.shape[1] < each:
         raise ValueError(f"page_table: {page_table.shape[1]} pages to a sequence, the call needs {each}")
-    return structs, len(tensors), NmsCachePages(_ptr(page_table, "int32", "page_table", 0), _int(page_table.shape[1], "page_table"),
-                                                  _int(slots, "tensors"), _int(count, "tensors"), 0)
+    if (count | slots | page_table.shape[1]) >> 31:
+        raise ValueError(f"page_table: {page_table.shape[1]} pages to a sequence, {count} pages of {slots} slots: they do not fit 32 bits")
+    return structs, len(tensors), NmsCachePages(_ptr(page_table, "int32", "page_table", 0), page_table.shape[1], slots, count, 0)
 
 
 def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, keep_out, kept_out, moves_out,
                            workspace, weights=None, valid_tokens=None, stream=None):
     """weights: [sequences, heads, group, tokens, columns], rows at one distance from each other, or None.
     moves_out: at least sequences * heads * (nms_cache_moves_max(n_max, budget) + 1) * 2 elements, or None."""
-    n, h, s, b = _cache_sizes(n_max, heads, sequences, budget)
+    n, h, s, b, first, recent = _cache_sizes(n_max, heads, sequences, budget, first, recent)
     _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
           "moves_out", moves_out, "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens)
     all_, s_ = _cache_elements(n, h, s)
@@ -747,16 +760,17 @@ def nms_cache_keep_batched(sums, positions, counts, lengths, n_max, heads, seque
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
     _check(lib.nms_cache_keep_batched(
         _ptr(sums, "float32", "sums", all_), _ptr(positions, "int32", "positions", all_), _ptr(counts, "int32", "counts", s_),
-        _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, _int(first, "first"), _int(recent, "recent"),
+        _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, first, recent,
         _ptr(keep_out, "uint8", "keep_out", all_), _ptr(kept_out, "int32", "kept_out", s_),
-        _ptr(moves_out, "int32", "moves_out", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ else 0), w, wb, _stream(stream)),
+        _ptr(moves_out, "int32", "moves_out", s_ * h * (max(nms_cache_moves_max(n, b), 0) + 1) * 2 if all_ and moves_out is not None else 0),
+        w, wb, _stream(stream)),
         "nms_cache_keep_batched")
 
 
 def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page_table=None, stream=None):
     """tensors: up to eight of shape [sequences, heads, n_max, row ...] (any strides whose rows are whole), or with a page table
     ([sequences, pages of a sequence] int32) [pages, heads, slots of a page, row ...]."""
-    n, h, s, b = _cache_sizes(n_max, heads, sequences, budget)
+    n, h, s, b, _, _ = _cache_sizes(n_max, heads, sequences, budget)
     tensors = tuple(tensors or ())  # gone over more than once
     _here("moves", moves, "page_table", page_table, *(x for t in tensors for x in ("tensors", t)))
     all_, s_ = _cache_elements(n, h, s)
@@ -767,7 +781,7 @@ def nms_cache_move_batched(moves, n_max, heads, sequences, budget, tensors, page
 
 def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, budget, first, recent, tensors, keep_out, kept_out,
                      workspace, weights, valid_tokens, page_table):
-    n, h, s, b = _cache_sizes(n_max, heads, sequences, budget)
+    n, h, s, b, first, recent = _cache_sizes(n_max, heads, sequences, budget, first, recent)
     tensors = tuple(tensors or ())  # gone over more than once
     _here("sums", sums, "positions", positions, "counts", counts, "lengths", lengths, "keep_out", keep_out, "kept_out", kept_out,
           "workspace", workspace, "weights", weights, "valid_tokens", valid_tokens, "page_table", page_table,
@@ -777,7 +791,7 @@ def _evict_arguments(sums, positions, counts, lengths, n_max, heads, sequences, 
     struct = _cache_weights(weights, valid_tokens, h, s) if all_ else None
     structs, many, pages = _cache_tensors(tensors if all_ else (), n, h, s, page_table)
     return (_ptr(sums, "float32", "sums", all_), _ptr(positions, "int32", "positions", all_), _ptr(counts, "int32", "counts", s_),
-            _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, _int(first, "first"), _int(recent, "recent"), structs, many, pages,
+            _ptr(lengths, "int32", "lengths", s_), n, h, s, struct, b, first, recent, structs, many, pages,
             _ptr(keep_out, "uint8", "keep_out", all_), _ptr(kept_out, "int32", "kept_out", s_), w, wb)
 
 
