@@ -73,8 +73,9 @@ extern "C" {
 
 typedef enum {
     NMS_OK = 0,
-    NMS_ERR_INVALID_ARG = -1,   /* null pointer, negative size, NaN threshold */
-    NMS_ERR_TOO_LARGE = -2,     /* n > NMS_MAX_N, frames > NMS_MAX_FRAMES, or the batch exceeds NMS_MAX_MAP_WORKGROUPS */
+    NMS_ERR_INVALID_ARG = -1,   /* null pointer, negative size, NaN threshold, outputs over inputs (decoding calls) */
+    NMS_ERR_TOO_LARGE = -2,     /* n > NMS_MAX_N, frames > NMS_MAX_FRAMES, the batch exceeds NMS_MAX_MAP_WORKGROUPS, or a size
+                                   the limits of a decoding call */
     NMS_ERR_WORKSPACE = -3,     /* workspace missing, misaligned or too small; nms_run without nms_init */
     NMS_ERR_LAUNCH = -4         /* the HIP runtime refused a launch */
 } nms_status;

@@ -13,7 +13,10 @@
 // compute unit has a row alone.
 //
 // Bound by: the rows' bytes for large batches (232 MB in 41 us of kernel time under the profiler, 47.5 to 49.1 us a call: 4.7 to 4.9 TB/s);
-// for small ones by the chain of dependent loads: token, its probabilities, row, entry (1 x 32,000 floats 9.0 us, 64 x 50,001 f16 4.9 + 5.0 us in two launches).
+// for small ones by the chain of dependent loads (token, its probabilities, row, entry: 1 x 32,000 floats 9.0 us, 64 x 50,001 f16 4.9 + 5.0 us in two
+// launches) and, where the vocabulary is no multiple of a segment, by the row's end, which goes element by element through 20 bytes of scratch
+// memory to a lane (up_to_end).  Calls, us: 1 x 30,720 floats 7.7, x 32,000 8.9, x 32,768 7.8; 64 x 49,152 / 50,001 / 51,200 f16 8.1 / 8.9 / 8.2;
+// 32 x 151,552 / 151,936 bf16 10.6 / 12.0; where the chip is full it does not show (256 x 151,111 / 151,552 floats 47.3 / 48.2).
 
 template <typename T>
 __device__ __forceinline__ float as_probability(T v)
@@ -127,7 +130,8 @@ struct __attribute__((packed, aligned(sizeof(T)))) Piece {  // 16 bytes at the a
     T v[16 / sizeof(T)];
 };
 
-// A piece at the row's end: 0 for what lies behind it.
+// A piece at the row's end: 0 for what lies behind it.  The branches keep the piece in scratch memory, and every piece of the last segment takes this
+// way, whole ones too: some 1.2 us of a short call.
 template <typename T>
 __device__ __forceinline__ Piece<T> up_to_end(const T *row, int at, int vocabulary)
 {

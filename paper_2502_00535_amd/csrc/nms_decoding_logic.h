@@ -61,6 +61,9 @@ static inline int nms_cache_vecs(int n_max, int frames)
 // The weights are added by the launch that finds the rows that stay where there are few query rows, by one of its own otherwise.  Whole call, us, with it /
 // on their own (bf16): 4 query rows, 8 x 4001 11.5 / 12.6, 512 x 2001 12.2 / 20.3; 16, 8 x 4001 16.9 / 13.2, 256 x 4001 23.4 / 23.9, 1024 x 1001 18.5 / 23.5;
 // 32, 8 x 4001 24.1 / 14.1, 256 x 4001 36.8 / 30.6, 1024 x 1001 27.8 / 29.7.
+// Between 8193 and 16,384 slots with 4 / 8 rows: f32, 8 x 12,000 16.2 / 13.2 and 20.4 / 13.4, 256 x 12,000 27.6 / 36.1 and 37.8 / 37.4; bf16, 8 x 12,000
+// 15.0 / 13.2 and 18.8 / 13.3, 256 x 12,000 21.4 / 38.7 and 28.2 / 39.5.  So the rule loses up to a third of a call where few long frames leave
+// compute units idle, and gains up to nine twentieths where they do not; f32 there spills 11 vector registers (the other instantiations none).
 static inline bool nms_cache_add_with_keep(int n_max, int frames, bool many_moves, long long rows)
 {
     return !nms_cache_split(n_max, frames, many_moves) && nms_cache_vecs(n_max, frames) <= 4 && (rows <= 8 || (rows <= 16 && frames >= 1024));
